@@ -420,7 +420,8 @@ int cod_selftest_expire_wait(cod_ctx* ctx, int on);
 
 /* Measurement aid (the paper has no counterpart): while class_mask has bit (1 << k) set,
    every launch of class k is bracketed by CUDA events on the launching stream (at most
-   4096 launches are recorded between two calls). class_mask = 0 switches it off.
+   4096 launches are recorded between two calls). class_mask = 0 switches it off. The first call
+   with another mask creates the events (host work of some milliseconds).
    Calling it also discards earlier records. */
 int cod_profile_enable(cod_ctx* ctx, uint32_t class_mask);
 /* Synchronises the recorded events and returns the summed duration and launch count of one

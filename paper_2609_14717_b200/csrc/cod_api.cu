@@ -141,6 +141,25 @@ bool scale_missing(const cod_ctx* c, const cod_state* s) { return c->kv8 && !s->
 bool other_device(const cod_ctx* c) { int d = -1; return cudaGetDevice(&d) != cudaSuccess || d != c->device; }
 bool hist_missing(const cod_ctx* c, const cod_state* s) { return c->carry_cap > c->cfg.block && !s->carry_hist; }
 
+// The records of cod_profile_enable: 8192 events take some two milliseconds to create, so a context has none before they are asked for.
+void drop_prof(cod_ctx* c) {
+  for (int i = 0; c->prof_ev && i < 2 * COD_PROF_SLOTS; ++i)
+    if (c->prof_ev[i]) cudaEventDestroy(c->prof_ev[i]);
+  free(c->prof_ev);
+  free(c->prof_class);
+  c->prof_ev = nullptr;
+  c->prof_class = nullptr;
+}
+bool make_prof(cod_ctx* c) {
+  if (c->prof_ev) return true;
+  c->prof_ev = static_cast<cudaEvent_t*>(calloc(2 * COD_PROF_SLOTS, sizeof(cudaEvent_t)));
+  c->prof_class = static_cast<unsigned char*>(calloc(COD_PROF_SLOTS, 1));
+  bool ok = c->prof_ev && c->prof_class;
+  for (int i = 0; ok && i < 2 * COD_PROF_SLOTS; ++i) ok = cudaEventCreate(&c->prof_ev[i]) == cudaSuccess;
+  if (!ok) { cudaGetLastError(); drop_prof(c); }
+  return ok;
+}
+
 int check_S(const cod_ctx* c, int S) { return (S >= 1 && S <= c->cfg.max_batch) ? COD_OK : COD_ERR_INVALID_ARG; }
 
 }  // namespace
@@ -258,14 +277,18 @@ int cod_create(const cod_config* cfg, cod_ctx** out) {
   }
   free(fr);
   free(frf);
-  c->prof_ev = static_cast<cudaEvent_t*>(calloc(2 * COD_PROF_SLOTS, sizeof(cudaEvent_t)));
-  c->prof_class = static_cast<unsigned char*>(calloc(COD_PROF_SLOTS, 1));
-  if (!c->prof_ev || !c->prof_class) ok = false;
   if (ok) ok = cudaStreamCreateWithFlags(&c->side, cudaStreamNonBlocking) == cudaSuccess &&
                cudaEventCreateWithFlags(&c->ev_fork, cudaEventDisableTiming) == cudaSuccess &&
                cudaEventCreateWithFlags(&c->ev_join, cudaEventDisableTiming) == cudaSuccess;
-  for (int i = 0; ok && i < 2 * COD_PROF_SLOTS; ++i) ok = cudaEventCreate(&c->prof_ev[i]) == cudaSuccess;
-  if (!ok) { cudaFree(c->ws); cudaGetLastError(); free(c->prof_ev); free(c->prof_class); delete c; return COD_ERR_CUDA; }
+  if (!ok) {
+    if (c->ev_fork) cudaEventDestroy(c->ev_fork);
+    if (c->ev_join) cudaEventDestroy(c->ev_join);
+    if (c->side) cudaStreamDestroy(c->side);
+    cudaFree(c->ws);
+    cudaGetLastError();
+    delete c;
+    return COD_ERR_CUDA;
+  }
   *out = c;
   return COD_OK;
 }
@@ -277,9 +300,7 @@ int cod_destroy(cod_ctx* c) {
   if (c->ev_fork) cudaEventDestroy(c->ev_fork);
   if (c->ev_join) cudaEventDestroy(c->ev_join);
   if (c->side) cudaStreamDestroy(c->side);
-  for (int i = 0; i < 2 * COD_PROF_SLOTS; ++i) cudaEventDestroy(c->prof_ev[i]);
-  free(c->prof_ev);
-  free(c->prof_class);
+  drop_prof(c);
   delete c;
   return COD_OK;
 }
@@ -707,7 +728,9 @@ int cod_selftest_expire_wait(cod_ctx* c, int on) {
 
 int cod_profile_enable(cod_ctx* c, uint32_t class_mask) {
   if (!c) return COD_ERR_INVALID_ARG;
-  c->prof_mask = class_mask & ((1u << COD_K_CLASSES) - 1u);
+  const uint32_t mask = class_mask & ((1u << COD_K_CLASSES) - 1u);
+  if (mask && (other_device(c) || !make_prof(c))) return COD_ERR_CUDA;
+  c->prof_mask = mask;
   c->prof_n = 0;
   return COD_OK;
 }

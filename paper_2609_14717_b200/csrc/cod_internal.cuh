@@ -202,7 +202,7 @@ struct cod_ctx {
   // optional per-kernel timing
   uint32_t prof_mask;
   int prof_n;
-  cudaEvent_t* prof_ev;        // [2 * COD_PROF_SLOTS], created at cod_create
+  cudaEvent_t* prof_ev;        // [2 * COD_PROF_SLOTS], null until cod_profile_enable asks for records
   unsigned char* prof_class;   // [COD_PROF_SLOTS]
 };
 
