@@ -194,24 +194,40 @@ class Split:
 
 
 class State:
-    """Paged committed KV, block table, carry slot and lengths of one batch (device tensors)."""
+    """Paged committed KV, block table, carry slot and lengths of one batch (device tensors).
 
-    def __init__(self, cfg: CodConfig, dtype: str, S: int, block_table: np.ndarray, committed_len: np.ndarray,
-                 device="cuda"):
+    block_table and committed_len: host arrays, or device tensors, which are used as they are. Tensors that the caller has
+    already (a pool, scales, carry slots) are used in the place of new ones, which start as zeros."""
+
+    def __init__(self, cfg: CodConfig, dtype: str, S: int, block_table, committed_len, device="cuda",
+                 kv_pool: Optional[torch.Tensor] = None, kv_scale: Optional[torch.Tensor] = None,
+                 carry_kv: Optional[torch.Tensor] = None, carry_len: Optional[torch.Tensor] = None,
+                 carry_hist: Optional[torch.Tensor] = None):
         td = torch_dtype(dtype)
         self.S = S
         kv8 = bool(cfg.flags & COD_F_KV8)                       # committed cache in e4m3 with one scale per page, head, K|V
-        self.kv_pool = torch.zeros((cfg.n_layers, cfg.n_pages, cfg.n_kv_heads, 2, cfg.page_size, cfg.head_dim),
-                                   dtype=torch.float8_e4m3fn if kv8 else td, device=device)
-        self.kv_scale = torch.zeros((cfg.n_layers, cfg.n_pages, cfg.n_kv_heads, 2), dtype=torch.float32,
-                                    device=device) if kv8 else None
-        self.block_table = torch.from_numpy(np.ascontiguousarray(block_table, dtype=np.int32)).to(device)
-        self.committed_len = torch.from_numpy(np.ascontiguousarray(committed_len, dtype=np.int32)).to(device)
         k = max(1, int(cfg.carry_rounds))                       # rounds of rejected rows the carry slot holds
-        self.carry_kv = torch.zeros((cfg.n_layers, cfg.max_batch, cfg.n_kv_heads, 2, k * cfg.block, cfg.head_dim),
-                                    dtype=td, device=device)
-        self.carry_len = torch.zeros(S, dtype=torch.int32, device=device)
-        self.carry_hist = torch.zeros((S, k), dtype=torch.int32, device=device) if k > 1 else None
+
+        def take(name, given, shape, dt):
+            if given is None:
+                return torch.zeros(shape, dtype=dt, device=device)
+            if given.dtype != dt or given.shape != shape:
+                raise ValueError(f"{name}: expected {dt} {shape}, got {given.dtype} {tuple(given.shape)}")
+            return given
+
+        def table(name, a, shape):
+            if isinstance(a, torch.Tensor) and a.is_cuda:
+                return take(name, a, shape, torch.int32)
+            return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(device)
+
+        self.kv_pool = take("kv_pool", kv_pool, (cfg.n_layers, cfg.n_pages, cfg.n_kv_heads, 2, cfg.page_size, cfg.head_dim),
+                            torch.float8_e4m3fn if kv8 else td)
+        self.kv_scale = take("kv_scale", kv_scale, (cfg.n_layers, cfg.n_pages, cfg.n_kv_heads, 2), torch.float32) if kv8 else None
+        self.block_table = table("block_table", block_table, (S, cfg.max_pages_per_seq))
+        self.committed_len = table("committed_len", committed_len, (S,))
+        self.carry_kv = take("carry_kv", carry_kv, (cfg.n_layers, cfg.max_batch, cfg.n_kv_heads, 2, k * cfg.block, cfg.head_dim), td)
+        self.carry_len = take("carry_len", carry_len, (S,), torch.int32)
+        self.carry_hist = take("carry_hist", carry_hist, (S, k), torch.int32) if k > 1 else None
 
     def struct(self) -> CodState:
         return CodState(*[_ptr(getattr(self, n)) for n in _STATE_FIELDS])
