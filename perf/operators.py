@@ -208,12 +208,15 @@ def prepare(case, seed):
         sh = synth.DrafterShape(d_target=8, n_cap=1, d_model=shape["n_q"] * shape["hd"], vocab=64, rope_theta=THETA,
                                 kv8=True, **shape)
         cfg = B.make_config(sh, S, width, n_pages)
-        st["ctx"] = B.Context(cfg)
-        own_state = B.State(cfg, sh.dtype, S, table, lens)
-        for mine, theirs in (("kv_pool", "pool"), ("kv_scale", "scale"), ("block_table", "table"), ("committed_len", "lens"),
-                             ("carry_kv", "carry"), ("carry_len", "carry_len")):
-            if theirs in st:
-                setattr(own_state, mine, st[theirs])
+        kept = prepare.__dict__.setdefault("contexts", {})            # a program makes a configuration's context once
+        if bytes(cfg) not in kept:
+            kept[bytes(cfg)] = B.Context(cfg)
+        st["ctx"] = kept[bytes(cfg)]
+        # the state over the tensors above; a pool that this operator does not touch is there in name only
+        pool = st["pool"] if "pool" in st else torch.empty((), dtype=torch.float8_e4m3fn, device="cuda").expand(1, n_pages, 1, 2, PAGE, 64)
+        scale = st["scale"] if "scale" in st else torch.empty((), device="cuda").expand(1, n_pages, 1, 2)
+        own_state = B.State(cfg, sh.dtype, S, st["table"], st["lens"], kv_pool=pool, kv_scale=scale, carry_kv=st.get("carry"),
+                            carry_len=st.get("carry_len"))
         st["state"] = own_state
         if op == "pages":
             st["pages"] = B.Pages(cfg, S, st["free_list"], st["n_free"], st["held"])
