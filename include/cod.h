@@ -166,7 +166,8 @@ typedef struct {
   int32_t* carry_hist;    /* [S][k] carry_rounds = k > 1 only (else may be NULL): lengths of the k
                                     newest rounds' segments of U_l, oldest first; starts as zeros   */
   float* kv_scale;        /* [Ld][n_pages][n_kv][2] COD_F_KV8 only (else may be NULL): scales of kv_pool's
-                                    pages. A page's scale is meaningless until a row is appended to it      */
+                                    pages, 8-byte aligned. A page's scale is meaningless until a row is
+                                    appended to it                                                          */
 } cod_state;
 
 /* Ownership of the pool's pages (device, caller-owned): the free pages as a stack, and how many entries of its row

@@ -136,7 +136,8 @@ int pick_splits(const cod_ctx* c, int n_out, int K, int rows) {
   return (kb + per - 1) / per;            // no empty split
 }
 
-bool scale_missing(const cod_ctx* c, const cod_state* s) { return c->kv8 && !s->kv_scale; }
+// the scales of a page's K and V are read as one float2
+bool scale_unusable(const cod_ctx* c, const cod_state* s) { return c->kv8 && (!s->kv_scale || (reinterpret_cast<uintptr_t>(s->kv_scale) & 7u)); }
 // the library's memory and kernels belong to the device that was current at cod_create
 bool other_device(const cod_ctx* c) { int d = -1; return cudaGetDevice(&d) != cudaSuccess || d != c->device; }
 bool hist_missing(const cod_ctx* c, const cod_state* s) { return c->carry_cap > c->cfg.block && !s->carry_hist; }
@@ -436,7 +437,7 @@ int cod_scatter_kv(cod_ctx* c, const void* J, const cod_split* split, int S, int
   if (check_S(c, S) != COD_OK || (mode != COD_CARRY && mode != COD_BASELINE)) return COD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   c->pdl = true;
-  if (hist_missing(c, st) || scale_missing(c, st)) return COD_ERR_INVALID_ARG;
+  if (hist_missing(c, st) || scale_unusable(c, st)) return COD_ERR_INVALID_ARG;
   int rc = COD_OK;
   if (c->carry_base && (rc = cod_launch_carry_age(c, split, S, mode, st, s)) != COD_OK) return rc;
   if ((rc = cod_launch_scatter(c, J, split, S, mode, st, s)) != COD_OK) return rc;
@@ -445,7 +446,7 @@ int cod_scatter_kv(cod_ctx* c, const void* J, const cod_split* split, int S, int
 
 int cod_kv_append(cod_ctx* c, const void* J, const int32_t* slot, int n_rows, cod_state* st, cod_stream_t stream) {
   if (!c || !J || !slot || !st || !st->kv_pool || misaligned(J) || misaligned(st->kv_pool)) return COD_ERR_INVALID_ARG;
-  if (n_rows < 1 || scale_missing(c, st) || other_device(c)) return COD_ERR_INVALID_ARG;
+  if (n_rows < 1 || scale_unusable(c, st) || other_device(c)) return COD_ERR_INVALID_ARG;
   c->pdl = true;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return c->kv8 ? cod_launch_kv8_append(c, J, slot, n_rows, st, s) : cod_launch_store_rows(c, J, slot, n_rows, st, s);
@@ -478,7 +479,7 @@ int cod_block_attn(cod_ctx* c, int layer, const void* q, const void* k_blk, cons
   if (misaligned(q) || misaligned(k_blk) || misaligned(v_blk) || misaligned(out) || misaligned(st->kv_pool) ||
       misaligned(st->carry_kv))
     return COD_ERR_INVALID_ARG;
-  if (check_S(c, S) != COD_OK || layer < 0 || layer >= c->cfg.n_layers || scale_missing(c, st)) return COD_ERR_INVALID_ARG;
+  if (check_S(c, S) != COD_OK || layer < 0 || layer >= c->cfg.n_layers || scale_unusable(c, st)) return COD_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   c->pdl = true;
   if (cod_attn_kv8_supported(c)) {          // rotates q and k_blk itself
@@ -519,7 +520,7 @@ static int round_impl(cod_ctx* c, const int32_t* draft, const int32_t* target, c
                       cod_state* st, cod_split* split_out, int32_t* next_draft, const cod_taps* taps,
                       cod_stream_t stream, float* q_next = nullptr, unsigned long long seed = 0, uint32_t step = 0) {
   const bool stochastic = p_tok != nullptr;
-  if (c && st && scale_missing(c, st)) return COD_ERR_INVALID_ARG;
+  if (c && st && scale_unusable(c, st)) return COD_ERR_INVALID_ARG;
   if (!c || (!stochastic && !draft) || !target || !H || !next_draft || state_has_null(st)) return COD_ERR_INVALID_ARG;
   if (stochastic && (!q_tok || !u)) return COD_ERR_INVALID_ARG;
   if (misaligned(H) || misaligned(st->kv_pool) || misaligned(st->carry_kv)) return COD_ERR_INVALID_ARG;
