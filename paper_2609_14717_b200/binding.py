@@ -158,6 +158,31 @@ def _want(name: str, t: torch.Tensor, dtype: str, shape) -> None:
         raise ValueError(f"{name}: expected {td} {shape}, got {t.dtype} {tuple(t.shape)}")
 
 
+def _arg(name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device: int) -> Optional[int]:
+    """Address of a tensor that holds at least the n elements which the call reaches, on the context's device."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected at least {n} contiguous elements of {dtype} on device {device}, "
+                         f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+_I32 = torch.int32
+
+
+class _Sizes:
+    """What a configuration says about its tensors, as plain numbers (a ctypes field costs a call of a few us 0.1 us per read)."""
+    __slots__ = ("device", "batch", "width", "rounds", "n_pages", "pool", "pool_dtype", "scales")
+
+    def __init__(self, cfg: CodConfig, device: int):
+        self.device, self.batch, self.width, self.n_pages = device, cfg.max_batch, cfg.max_pages_per_seq, cfg.n_pages
+        self.rounds = max(1, cfg.carry_rounds)
+        self.scales = cfg.n_layers * cfg.n_pages * cfg.n_kv_heads * 2
+        self.pool = self.scales * cfg.page_size * cfg.head_dim
+        self.pool_dtype = (torch.float8_e4m3fn if cfg.flags & COD_F_KV8 else torch.bfloat16 if cfg.dtype == COD_BF16 else torch.float32)
+
+
 def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
@@ -232,14 +257,18 @@ class State:
     def struct(self) -> CodState:
         return CodState(*[_ptr(getattr(self, n)) for n in _STATE_FIELDS])
 
-    def cache_struct(self) -> CodState:
+    def cache_struct(self, sizes: _Sizes) -> CodState:
         """The fields that cod_kv_append reads (marshalling a tensor costs the host some 0.4 us, a small append's kernel takes 4)."""
-        return CodState(kv_pool=_ptr(self.kv_pool), kv_scale=_ptr(self.kv_scale))
+        return CodState(_arg("kv_pool", self.kv_pool, sizes.pool, sizes.pool_dtype, sizes.device), None, None, None, None, None,
+                        _arg("kv_scale", self.kv_scale, sizes.scales, torch.float32, sizes.device))
 
-    def table_struct(self) -> CodState:
+    def table_struct(self, sizes: _Sizes, S: int) -> CodState:
         """The fields that cod_pages_reserve and cod_pages_release read and write."""
-        return CodState(block_table=_ptr(self.block_table), committed_len=_ptr(self.committed_len), carry_len=_ptr(self.carry_len),
-                        carry_hist=_ptr(self.carry_hist))
+        dev, width = sizes.device, sizes.width
+        if self.block_table.shape[-1] != width:
+            raise ValueError(f"block_table: expected rows of {width}, got {tuple(self.block_table.shape)}")
+        return CodState(None, _arg("block_table", self.block_table, S * width, _I32, dev), _arg("committed_len", self.committed_len, S, _I32, dev),
+                        None, _arg("carry_len", self.carry_len, S, _I32, dev), _arg("carry_hist", self.carry_hist, S * sizes.rounds, _I32, dev))
 
 
 class Pages:
@@ -252,8 +281,10 @@ class Pages:
         self.n_free = n_free if n_free is not None else torch.full((1,), cfg.n_pages, **i32)
         self.held = held if held is not None else torch.zeros(S, **i32)
 
-    def struct(self) -> CodPages:
-        return CodPages(*[_ptr(getattr(self, n)) for n in _PAGES_FIELDS])
+    def struct(self, sizes: _Sizes, S: int) -> CodPages:
+        dev = sizes.device
+        return CodPages(_arg("free_list", self.free_list, sizes.n_pages, _I32, dev), _arg("n_free", self.n_free, 1, _I32, dev),
+                        _arg("held", self.held, S, _I32, dev))
 
 
 class RowPlan:
@@ -267,8 +298,10 @@ class RowPlan:
         self.row_pos = torch.full((max_rows,), -1, **i32)
         self.row_seq = torch.full((max_rows,), -1, **i32)
 
-    def struct(self) -> CodRowPlan:
-        return CodRowPlan(*[_ptr(getattr(self, n)) for n in _PLAN_FIELDS], self.max_rows)
+    def struct(self, sizes: _Sizes, S: int) -> CodRowPlan:
+        dev, n = sizes.device, self.max_rows
+        return CodRowPlan(_arg("row_off", self.row_off, S + 1, _I32, dev), _arg("slot", self.slot, n, _I32, dev),
+                          _arg("row_pos", self.row_pos, n, _I32, dev), _arg("row_seq", self.row_seq, n, _I32, dev), n)
 
 
 class Taps:
@@ -295,6 +328,7 @@ class Context:
         torch.zeros(1, device="cuda")          # make sure the primary context exists
         self.cfg = cfg
         self.dtype = "bf16" if cfg.dtype == COD_BF16 else "f32"
+        self._sizes = _Sizes(cfg, torch.cuda.current_device())
         self._h = C.c_void_p()
         _check("cod_create", lib().cod_create(C.byref(cfg), C.byref(self._h)))
         self._weights = None
@@ -332,26 +366,30 @@ class Context:
 
     def kv_append(self, J, slot, state: State) -> None:
         """J [Ld, n_rows, 2, n_kv, hd] into the committed cache at slot [n_rows] (-1: nowhere)."""
-        _want("J", J, self.dtype, (self.cfg.n_layers, slot.numel(), 2, self.cfg.n_kv_heads, self.cfg.head_dim))
-        _want("slot", slot, "i32", (slot.numel(),))
-        st = state.cache_struct()
-        _check("cod_kv_append", lib().cod_kv_append(self._h, _ptr(J), _ptr(slot), slot.numel(), C.byref(st), _stream()))
+        sz, n = self._sizes, slot.numel()
+        _want("J", J, self.dtype, (self.cfg.n_layers, n, 2, self.cfg.n_kv_heads, self.cfg.head_dim))
+        _check("cod_kv_append", lib().cod_kv_append(self._h, _arg("J", J, 0, J.dtype, sz.device), _arg("slot", slot, n, _I32, sz.device), n,
+                                                    state.cache_struct(sz), _stream()))
 
     def pages_reserve(self, pages: Pages, n_new, state: State, S, plan: Optional[RowPlan] = None,
                       advance: bool = False) -> None:
         """Pages for n_new [S] more tokens per sequence; plan: where their rows go; advance: the lengths grow too."""
-        _want("n_new", n_new, "i32", (S,))
-        st, pg = state.table_struct(), pages.struct()
-        pl = plan.struct() if plan is not None else None
+        sz = self._sizes
+        n = S if S <= sz.batch else sz.batch                    # (a larger S is refused by the library)
+        if n_new.numel() != S:
+            raise ValueError(f"n_new: expected {S} elements, got {tuple(n_new.shape)}")
         _check("cod_pages_reserve", lib().cod_pages_reserve(
-            self._h, C.byref(pg), _ptr(n_new), S, C.byref(st), C.byref(pl) if pl is not None else None, int(advance), _stream()))
+            self._h, pages.struct(sz, n), _arg("n_new", n_new, S, _I32, sz.device), S, state.table_struct(sz, n),
+            plan.struct(sz, n) if plan is not None else None, int(advance), _stream()))
 
     def pages_release(self, pages: Pages, keep, state: State, S) -> None:
         """Pages behind the first keep [S] tokens back to the free list (keep None: behind the committed ones)."""
-        if keep is not None:
-            _want("keep", keep, "i32", (S,))
-        st, pg = state.table_struct(), pages.struct()
-        _check("cod_pages_release", lib().cod_pages_release(self._h, C.byref(pg), _ptr(keep), S, C.byref(st), _stream()))
+        sz = self._sizes
+        n = S if S <= sz.batch else sz.batch
+        if keep is not None and keep.numel() != S:
+            raise ValueError(f"keep: expected {S} elements, got {tuple(keep.shape)}")
+        _check("cod_pages_release", lib().cod_pages_release(
+            self._h, pages.struct(sz, n), _arg("keep", keep, S, _I32, sz.device), S, state.table_struct(sz, n), _stream()))
 
     def block_attn(self, layer, q, k_blk, v_blk, state: State, S, use_carry, out, carry_mass=None) -> None:
         st = state.struct()
