@@ -105,7 +105,7 @@ enum cod_mode {
 #define COD_DEV_TIMEOUT 8u        /* a bounded device-side wait gave up */
 #define COD_DEV_BAD_LEN 16u       /* committed_len / carry_len outside its range; a negative n_new or keep; held or n_free outside its range */
 #define COD_DEV_NO_PAGES 32u      /* cod_pages_reserve: the free list ran out, at least one sequence got nothing */
-#define COD_DEV_BAD_SLOT 64u      /* cod_kv_append: a slot beyond the pool, or rows of a page out of order (row not stored) */
+#define COD_DEV_BAD_SLOT 64u      /* cod_kv_append: a slot beyond the pool, or a row that breaks its page's run (row not stored) */
 
 /* Immutable description of the drafter and of the capacities the workspace is sized for. */
 typedef struct {
@@ -267,10 +267,13 @@ int cod_scatter_kv(cod_ctx* ctx, const void* J, const cod_split* split, int S, i
    slot [n_rows] device int32: page*page_size + offset, or -1 for a row that goes nowhere (cod_row_plan.slot, or
    cod_split.commit_slot). Any n_rows >= 1; lengths are not touched (see cod_pages_reserve's advance). Of st only
    kv_pool and kv_scale are used.
-   COD_F_KV8: rows are quantised. The rows of one page must lie one behind the other in increasing order of slot, as
-   they do in both of those maps, a page may occur in one place of the map only, and what the page holds below its
-   first new row is kept; a page whose offset 0 is written starts afresh. A row that breaks the order inside its page is
-   skipped with COD_DEV_BAD_SLOT, as is a slot beyond the pool. */
+   COD_F_KV8: rows are quantised. The rows of one page must lie next to each other in the map with consecutive slots (no
+   -1 among them), as they do in both of those maps, a page may occur in one place of the map only, and what the page holds
+   below its first new row is kept; a page whose offset 0 is written starts afresh. A row of the same page as the nearest
+   earlier row that goes somewhere, which does not follow it at once, is skipped with COD_DEV_BAD_SLOT, with the rows
+   that follow it in that page; so is a slot beyond the pool. A page that occurs again after rows of other pages is not
+   noticed, and what it then holds is undefined (both runs rescale it), like a slot that occurs twice in a cache of
+   the storage type. */
 int cod_kv_append(cod_ctx* ctx, const void* J, const int32_t* slot, int n_rows, cod_state* st,
                   cod_stream_t stream);
 

@@ -73,6 +73,7 @@ template <> struct Raw8<float> {
 
 // Block (x, y) = (chunk of `chunk` rows, layer). A row is a leader if it opens its page's run of rows: the first row,
 // offset 0, or a row that does not follow its predecessor. Leaders x (head, K|V) are dealt to the block's warps.
+// (A page that occurs again after another page's rows would have two owners unseen: finding those takes a pass over the whole map.)
 // LONG: what bounds a long map is how many rows are on their way, so registers give way to a fourth block per SM (bf16; 25,000
 // rows of five layers: 142 us, with three blocks 152, with five, which spill, 147; its bytes at the rate of a plain copy: 132).
 // A short map fits the machine at once and keeps them (a round's rows at batch 32: 7.5 us).
@@ -86,19 +87,34 @@ k_kv8_append(const T* __restrict__ J, const int* __restrict__ slot, int n_rows, 
   const int row0 = blockIdx.x * chunk, layer = blockIdx.y;
   const long long n_slots = static_cast<long long>(n_pages) * PAGE;
   if (warp == 0) {
-    const int r = row0 + lane;
-    bool opens = false;
-    if (lane < chunk && r < n_rows) {
-      const int sl = slot[r], prev = r > 0 ? slot[r - 1] : -1;
-      if (sl >= 0) {
-        const bool follows = prev >= 0 && prev == sl - 1 && (sl & (PAGE - 1)) != 0;
-        opens = !follows;
-        // a row of its predecessor's page that does not follow it would be a second owner of that page
-        if (sl >= n_slots || (opens && prev >= 0 && prev / PAGE == sl / PAGE)) {
-          if (layer == 0) atomicOr(status, COD_DEV_BAD_SLOT);
-          opens = false;
+    const int r = row0 + lane, w = row0 - 32 + lane;
+    const int sl = lane < chunk && r < n_rows ? slot[r] : -1, old = w >= 0 ? slot[w] : -1;
+    const unsigned here = __ballot_sync(0xffffffffu, sl >= 0), past = __ballot_sync(0xffffffffu, old >= 0);
+    const unsigned below = here & ((1u << lane) - 1u);
+    const int in_chunk = __shfl_sync(0xffffffffu, sl, below ? 31 - __clz(below) : 0);
+    const int in_past = __shfl_sync(0xffffffffu, old, past ? 31 - __clz(past) : 0);
+    int before = below ? in_chunk : past ? in_past : -1;     // the nearest earlier row that goes somewhere
+    const bool next_to_it = lane ? (here >> (lane - 1)) & 1u : past >> 31;
+    bool opens = sl >= 0 && !(next_to_it && before == sl - 1 && (sl & (PAGE - 1)) != 0);
+    if (past == 0 && __any_sync(0xffffffffu, opens)) {       // rows that go nowhere, more than 32 of them: further back
+      int found = -1;
+      for (int end = row0 - 32; found < 0 && end > 0; end -= 256) {
+        int v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { const int at = end - 256 + 32 * u + lane; v[u] = at >= 0 ? slot[at] : -1; }
+#pragma unroll
+        for (int u = 7; u >= 0; --u) {
+          const unsigned some = __ballot_sync(0xffffffffu, v[u] >= 0);
+          const int last = __shfl_sync(0xffffffffu, v[u], some ? 31 - __clz(some) : 0);
+          if (found < 0 && some) found = last;
         }
       }
+      if (!below) before = found;
+    }
+    // a row of its predecessor's page that does not follow it would be a second owner of that page
+    if (opens && (sl >= n_slots || (before >= 0 && before / PAGE == sl / PAGE))) {
+      if (layer == 0) atomicOr(status, COD_DEV_BAD_SLOT);
+      opens = false;
     }
     const unsigned m = __ballot_sync(0xffffffffu, opens);
     if (opens) lead[__popc(m & ((1u << lane) - 1u))] = r;

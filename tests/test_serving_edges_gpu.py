@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_kv8_gpu import _B, _ctx
+from tests import kv8_ref as ref
+from tests.test_kv8_gpu import _B, _check_bytes, _ctx, _i32, _values
 
 pytestmark = pytest.mark.gpu
 
@@ -79,3 +80,31 @@ def test_tensors_of_fewer_sequences_pages_or_rows_do_not_reach_the_device():
     ctx.pages_reserve(pages, n, st, 4, plan)                     # and what fits goes through
     assert ctx.poll_status() == 0 and plan.row_off.tolist() == [0, 1, 2, 3, 4]
     ctx.close()
+
+
+# ----------------------------------------------------------------------------- append
+@pytest.mark.parametrize("layers,dtype", [(1, "bf16"), (3, "f32")])
+@pytest.mark.parametrize("case", ["hole", "hole_later", "backwards", "start_again", "wide_hole", "far", "farther", "fine"])
+def test_append_skips_what_follows_a_hole_in_its_own_page(case, layers, dtype):
+    """Rows that go nowhere between two rows of one page: the second part would be a second owner of the page. It is skipped and
+    reported; the rest of the map, and the page's first part, are stored as if it were not there."""
+    B = _B()
+    n = {"far": 300, "farther": 6000, "wide_hole": 33}.get(case, 2)
+    one = {"hole": [18, -1, 19], "hole_later": [16, 17, 18, 19, -1, -7, 22, 23], "backwards": [21, -1, 17, 18], "start_again": [21, 22, -1, 16, 17],
+           "fine": [18, 19, 20, -1, 48, 49, -1, -1, 33, 34]}.get(case, [18] + [-1] * n + [25, 26])
+    keep = {"hole": 1, "hole_later": 6, "backwards": 1, "start_again": 2, "fine": 10}.get(case, 1)
+    rng = np.random.default_rng(len(one))
+    for lead in (0, 1, 3, 15, 40):                             # where the break lies in the blocks' chunks of rows
+        head = list(range(64 + 9, 64 + 9 + lead)) if lead < 40 else list(range(64, 64 + lead))
+        bad = head + one + [112, 113, -1, 128]
+        good = list(head) + one[:keep] + [-1] * (len(one) - keep) + [112, 113, -1, 128]
+        ctx, st, _ = _ctx(S=1, W=1, n_q=2, n_kv=2, hd=64, layers=layers, n_pages=12, dtype=dtype)
+        st.kv_pool.view(torch.uint8).copy_(torch.from_numpy(rng.integers(0, 0x7F, size=tuple(st.kv_pool.shape), dtype=np.uint8)))
+        st.kv_scale.copy_(torch.from_numpy(2.0 ** rng.integers(-6, 1, size=tuple(st.kv_scale.shape)).astype(np.float64)))
+        J = torch.from_numpy(rng.normal(size=(layers, len(bad), 2, 2, 64))).to(torch.bfloat16 if dtype == "bf16" else torch.float32).cuda()
+        pool, scale = _values(st.kv_pool), _values(st.kv_scale)
+        ctx.kv_append(J, _i32(bad), st)
+        ref.append(pool, scale, _values(J), np.array(good))
+        _check_bytes(st, pool, scale)
+        assert ctx.poll_status() == (0 if case == "fine" else B.DEV_BAD_SLOT)
+        ctx.close()
