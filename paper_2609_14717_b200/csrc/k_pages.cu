@@ -6,6 +6,7 @@
 // release: first[s] = min(held, ceil(keep / page)); with E the prefix sum of held - first and T its total, the page at
 //   place first + i goes to free_list[n_free + T - 1 - (E[s] + i)]: the stack then hands the same pages out again in
 //   the same order.
+// A sequence whose numbers are out of range (a negative length, held beyond the table) is refused: nothing of it changes.
 //
 // A few words per page and row: bound by latency (dependent trips to L2), not by bytes (release and reserve of a round at
 // batch 32: 8.4 us on the device; admission of 64 prompts with 60,000 row slots: 11.6 us). One launch: every block
@@ -29,7 +30,7 @@ struct PagesArgs {
   int S, page, max_pages, n_pages, hist_len, advance;
   int *row_off, *slot, *row_pos, *row_seq;
   int max_rows;
-  unsigned int* ticket;
+  unsigned int* ticket;       // [0] blocks that are done, [1] release: a table held something that is no page
   uint32_t* status;
 };
 
@@ -85,7 +86,8 @@ __global__ void __launch_bounds__(PT) k_pages_reserve(const PagesArgs a) {
   constexpr int REFUSED = 1 << 30;
   uint32_t flags = 0;
   int nf = *a.n_free;
-  if (nf < 0 || nf > a.n_pages) { flags |= COD_DEV_BAD_LEN; nf = max(0, min(nf, a.n_pages)); }
+  const bool list_ok = nf >= 0 && nf <= a.n_pages;       // else nothing is handed out and n_free stays
+  if (!list_ok) { flags |= COD_DEV_BAD_LEN; nf = 0; }
   long long pages_before = 0, rows_before = 0;
   int granted = 0;                      // pages handed out to the sequences so far
   for (int s0 = 0; s0 < a.S; s0 += PT) {
@@ -132,18 +134,20 @@ __global__ void __launch_bounds__(PT) k_pages_reserve(const PagesArgs a) {
     if (pg < 0 || pg >= a.n_pages) { flags |= COD_DEV_BAD_PAGE; return -1; }
     return pg;
   };
-  for (int r = tid; r < granted; r += nt) {
+  for (long long at = tid; at < granted; at += nt) {
+    const int r = static_cast<int>(at);
     // sequences without a need share their rank with the next one: the last of equals owns it, unless it was refused
     int s = owner(pfx, a.S, r);
     a.block_table[static_cast<size_t>(s) * a.max_pages + (hold[s] & ~REFUSED) + (r - pfx[s])] = page_of(r);
   }
   if (a.slot != nullptr) {
-    for (int r = tid; r < a.max_rows; r += nt) {
+    for (long long at = tid; at < a.max_rows; at += nt) {
+      const int r = static_cast<int>(at);
       int sl = -1, pos = -1, sq = -1;
       if (r < rows) {
         sq = owner(roff, a.S, r);
         const int L = a.committed_len[sq], h = hold[sq];
-        pos = L + (r - roff[sq]);
+        pos = static_cast<int>(min(L + static_cast<long long>(r - roff[sq]), 0x7FFFFFFFll));   // (beyond it: a refused sequence's)
         if (!(h & REFUSED)) {
           const int place = pos / a.page;
           const int pg = place < h ? a.block_table[static_cast<size_t>(sq) * a.max_pages + place] : page_of(pfx[sq] + place - h);
@@ -167,7 +171,10 @@ __global__ void __launch_bounds__(PT) k_pages_reserve(const PagesArgs a) {
     if (want > h) a.held[s] = want;
     if (a.advance) a.committed_len[s] = L + n;
   }
-  if (threadIdx.x == 0) { *a.n_free = nf - granted; *a.ticket = 0; }
+  if (threadIdx.x == 0) {
+    if (list_ok) *a.n_free = nf - granted;
+    *a.ticket = 0;
+  }
 }
 
 __global__ void __launch_bounds__(PT) k_pages_release(const PagesArgs a) {
@@ -175,21 +182,23 @@ __global__ void __launch_bounds__(PT) k_pages_release(const PagesArgs a) {
   extern __shared__ int sm[];
   __shared__ long long red[PT / 32];
   int* pfx = sm;                        // [S] rank of the first page that goes
-  int* first = sm + a.S;                // [S] its place in the table
+  int* first = sm + a.S;                // [S] its place in the table; -1: refused
   uint32_t flags = 0;
   int nf = *a.n_free;
-  if (nf < 0 || nf > a.n_pages) { flags |= COD_DEV_BAD_LEN; nf = max(0, min(nf, a.n_pages)); }
+  const bool list_ok = nf >= 0 && nf <= a.n_pages;       // else every sequence is refused
+  if (!list_ok) { flags |= COD_DEV_BAD_LEN; nf = 0; }
   long long before = 0;
   for (int s0 = 0; s0 < a.S; s0 += PT) {
     const int s = s0 + threadIdx.x;
     long long gone = 0;
-    int f = 0;
+    int f = -1;
     if (s < a.S) {
-      int keep = a.len_in ? a.len_in[s] : a.committed_len[s], h = a.held[s];
-      if (keep < 0) { flags |= COD_DEV_BAD_LEN; keep = 0; }
-      if (h < 0 || h > a.max_pages) { flags |= COD_DEV_BAD_LEN; h = max(0, min(h, a.max_pages)); }
-      f = min(h, keep / a.page + (keep % a.page ? 1 : 0));
-      gone = h - f;
+      const int L = a.committed_len[s], keep = a.len_in ? a.len_in[s] : L, h = a.held[s];
+      if (L < 0 || keep < 0 || h < 0 || h > a.max_pages) flags |= COD_DEV_BAD_LEN;
+      else if (list_ok) {
+        f = min(h, keep / a.page + (keep % a.page ? 1 : 0));
+        gone = h - f;
+      }
     }
     long long tot;
     const long long e = before + block_scan(gone, red, tot);
@@ -199,18 +208,38 @@ __global__ void __launch_bounds__(PT) k_pages_release(const PagesArgs a) {
   __syncthreads();
   const int total = static_cast<int>(before);
   const int tid = blockIdx.x * PT + threadIdx.x, nt = gridDim.x * PT;
-  for (int r = tid; r < total; r += nt) {
-    const int s = owner(pfx, a.S, r);
+  bool hole = false;
+  for (long long r = tid; r < total; r += nt) {          // (table and list may each hold 2^31 - 1 entries)
+    const int s = owner(pfx, a.S, static_cast<int>(r));
     int* e = a.block_table + static_cast<size_t>(s) * a.max_pages + first[s] + (r - pfx[s]);
-    const int pg = *e, at = nf + total - 1 - r;
-    if (pg < 0 || pg >= a.n_pages) flags |= COD_DEV_BAD_PAGE;
+    const int pg = *e;
+    const long long at = nf + static_cast<long long>(total) - 1 - r;
+    if (pg < 0 || pg >= a.n_pages) { flags |= COD_DEV_BAD_PAGE; hole = true; }
     if (at < a.n_pages) a.free_list[at] = pg; else flags |= COD_DEV_BAD_PAGE;    // more pages than there are: some came twice
     *e = -1;
   }
+  if (hole) atomicOr(a.ticket + 1, 1u);
   if (flags) atomicOr(a.status, flags);
   if (!last_block(a.ticket)) return;
+  int top = static_cast<int>(min(nf + static_cast<long long>(total), static_cast<long long>(a.n_pages)));
+  if (*static_cast<volatile unsigned int*>(a.ticket + 1)) {   // what is no page does not stay on the list: one warp closes the gaps
+    if (threadIdx.x < 32) {
+      const int lane = threadIdx.x;
+      int to = nf;
+      for (long long i = nf; i < top; i += 32) {
+        const int pg = i + lane < top ? *static_cast<volatile int*>(a.free_list + i + lane) : -1;
+        const bool is_page = pg >= 0 && pg < a.n_pages;
+        const unsigned m = __ballot_sync(0xffffffffu, is_page);         // (every lane has read before one writes: the places it
+        if (is_page) a.free_list[to + __popc(m & ((1u << lane) - 1u))] = pg;      // writes lie at or below those of this step)
+        to += __popc(m);
+        __syncwarp();
+      }
+      top = to;
+    }
+  }
   for (int s = threadIdx.x; s < a.S; s += PT) {
-    const int keep = a.len_in ? max(0, a.len_in[s]) : 0x7FFFFFFF, L = a.committed_len[s];
+    if (first[s] < 0) continue;
+    const int keep = a.len_in ? a.len_in[s] : 0x7FFFFFFF, L = a.committed_len[s];
     a.held[s] = first[s];
     if (keep < L) {
       a.committed_len[s] = keep;
@@ -218,7 +247,11 @@ __global__ void __launch_bounds__(PT) k_pages_release(const PagesArgs a) {
       if (a.carry_hist) for (int j = 0; j < a.hist_len; ++j) a.carry_hist[static_cast<size_t>(s) * a.hist_len + j] = 0;
     }
   }
-  if (threadIdx.x == 0) { *a.n_free = min(nf + total, a.n_pages); *a.ticket = 0; }
+  if (threadIdx.x == 0) {
+    if (list_ok) *a.n_free = top;
+    a.ticket[0] = 0;
+    a.ticket[1] = 0;
+  }
 }
 
 PagesArgs common_args(cod_ctx* c, const cod_pages* pages, const int32_t* len_in, int S, const cod_state* st) {

@@ -108,3 +108,89 @@ def test_append_skips_what_follows_a_hole_in_its_own_page(case, layers, dtype):
         _check_bytes(st, pool, scale)
         assert ctx.poll_status() == (0 if case == "fine" else B.DEV_BAD_SLOT)
         ctx.close()
+
+
+# ----------------------------------------------------------------------------- page tables
+def _held_state(S=4, width=6, n_pages=40, carry_rounds=2, lens=(20, 33, 5, 40)):
+    """Four sequences with pages for their tokens and for a block behind them, and carried rows."""
+    B = _B()
+    ctx, st, cfg = _ctx(S=S, width=width, n_pages=n_pages, carry_rounds=carry_rounds)
+    pages = B.Pages(cfg, S)
+    t = ref.Tables(n_pages, S, width, [0] * S)
+    ctx.pages_reserve(pages, _i32(lens), st, S, advance=True)
+    t.reserve(lens, advance=True)
+    ctx.pages_reserve(pages, _i32([16] * S), st, S)
+    t.reserve([16] * S)
+    st.carry_len.fill_(3)
+    st.carry_hist.fill_(1)
+    assert ctx.poll_status() == 0
+    return ctx, st, cfg, pages, t
+
+
+def _all_of(st, pages):
+    return {k: v.clone() for k, v in (("table", st.block_table), ("lens", st.committed_len), ("carry_len", st.carry_len), ("hist", st.carry_hist),
+                                      ("free", pages.free_list), ("n_free", pages.n_free), ("held", pages.held))}
+
+
+@pytest.mark.parametrize("what", ["keep", "held_above", "held_below", "length"])
+def test_release_leaves_a_sequence_with_bad_numbers_as_it_was(what):
+    """The other sequences are served as ever; of the bad one nothing moves, and only pages that exist are on the free list."""
+    B = _B()
+    ctx, st, cfg, pages, t = _held_state()
+    keep = [0, -1 if what == "keep" else 20, 5, 17]
+    if what.startswith("held"):
+        pages.held[1] = 99 if what == "held_above" else -2
+    if what == "length":
+        st.committed_len[1] = -7
+    was = _all_of(st, pages)
+    ctx.pages_release(pages, _i32(keep), st, 4)
+    assert ctx.poll_status() == B.DEV_BAD_LEN
+    now = _all_of(st, pages)
+    for k in ("table", "lens", "carry_len", "hist", "held"):
+        assert torch.equal(now[k][1], was[k][1]), k
+    gone = []
+    for s, first in ((0, 0), (2, 1), (3, 2)):
+        gone += t.table[s][first:t.held[s]]
+        assert now["table"][s].tolist() == t.table[s][:first] + [-1] * (6 - first) and now["held"][s] == first
+    assert now["lens"].tolist() == [0, int(was["lens"][1]), 5, 17] and now["carry_len"].tolist() == [0, 3, 3, 0]
+    assert now["hist"].tolist() == [[0, 0], [1, 1], [1, 1], [0, 0]]
+    want = t.free + gone[::-1]
+    assert int(now["n_free"]) == len(want) and now["free"][:len(want)].tolist() == want
+    ctx.close()
+
+
+def test_what_is_no_page_does_not_come_onto_the_free_list():
+    """Table entries that were overwritten: reported, left out, and the list has no hole; its pages can be handed out again."""
+    B = _B()
+    ctx, st, cfg, pages, t = _held_state(S=4, width=40, n_pages=200, lens=(600, 33, 500, 40))
+    rng = np.random.default_rng(3)
+    for s, n in ((0, 5), (2, 30), (3, 1)):
+        for j in rng.permutation(t.held[s])[:n]:
+            t.table[s][j] = int(rng.choice([-1, -9, 200, 2 ** 31 - 1]))
+    st.block_table.copy_(_i32(t.table))
+    ctx.pages_release(pages, _i32([0, 33, 0, 0]), st, 4)
+    assert ctx.poll_status() == B.DEV_BAD_PAGE
+    gone = [p for s, first in ((0, 0), (1, 3), (2, 0), (3, 0)) for p in t.table[s][first:t.held[s]] if 0 <= p < 200]
+    want = t.free + gone[::-1]
+    assert int(pages.n_free) == len(want) == 200 - 3 - 36
+    assert pages.free_list[:len(want)].tolist() == want and pages.held.tolist() == [0, 3, 0, 0]
+    ctx.pages_release(pages, None, st, 4)                        # nothing is left over from the report
+    assert ctx.poll_status() == 0 and int(pages.n_free) == len(want)
+    ctx.pages_reserve(pages, _i32([0, 0, 600, 0]), st, 4)
+    assert ctx.poll_status() == 0 and st.block_table[2, :38].tolist() == want[::-1][:38]
+    ctx.close()
+
+
+@pytest.mark.parametrize("n_free", [-1, 41])
+def test_a_free_list_of_an_impossible_length_is_left_alone(n_free):
+    B = _B()
+    ctx, st, cfg, pages, t = _held_state()
+    pages.n_free.fill_(n_free)
+    was = _all_of(st, pages)
+    ctx.pages_release(pages, _i32([0, 0, 0, 0]), st, 4)
+    assert ctx.poll_status() == B.DEV_BAD_LEN
+    ctx.pages_reserve(pages, _i32([40, 1, 1, 1]), st, 4, advance=False)
+    assert ctx.poll_status() == B.DEV_BAD_LEN | B.DEV_NO_PAGES
+    for k, v in _all_of(st, pages).items():
+        assert torch.equal(v, was[k]), k
+    ctx.close()
