@@ -288,9 +288,9 @@ int cod_kv_append(cod_ctx* ctx, const void* J, const int32_t* slot, int n_rows, 
    += n_new[s] for the served sequences, for callers that append those rows next.
    release: sequence s keeps its first keep[s] tokens: pages held beyond ceil(keep[s] / page_size) go back onto the free
    list (their table entries become -1) in an order in which reserving them again at once gives the same table back;
-   where keep[s] < committed_len[s] that becomes the length, and the carried rows, which follow tokens that are gone,
-   are dropped (carry_len[s] = 0, carry_hist[s] = 0). keep [S] device int32, or NULL: committed_len, i.e. only what is reserved and unused
-   goes back. keep = 0 ends a request. Both refuse a sequence with a negative length, n_new or keep, or with held outside
+   where keep[s] < committed_len[s], or keep[s] = 0, that becomes the length, and the carried rows, which follow tokens that
+   are gone, are dropped (carry_len[s] = 0, carry_hist[s] = 0). keep [S] device int32, or NULL: committed_len, i.e. only
+   what is reserved and unused goes back and the carried rows stay. keep[s] = 0 ends a request. Both refuse a sequence with a negative length, n_new or keep, or with held outside
    0 .. max_pages_per_seq (COD_DEV_BAD_LEN), and leave it as it was; with n_free outside 0 .. n_pages no page moves at all. What is
    no page (a table entry outside 0 .. n_pages-1) never comes onto the free list (COD_DEV_BAD_PAGE). Sequences are the first S rows of the state's arrays, S <= 4096
    (COD_ERR_TOO_LARGE). Of st they use block_table, committed_len, carry_len and carry_hist only. */

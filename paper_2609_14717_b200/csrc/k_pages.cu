@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(PT) k_pages_release(const PagesArgs a) {
     if (first[s] < 0) continue;
     const int keep = a.len_in ? a.len_in[s] : 0x7FFFFFFF, L = a.committed_len[s];
     a.held[s] = first[s];
-    if (keep < L) {
+    if (keep < L || keep == 0) {        // (a request of no tokens that ends may have carried rows, too)
       a.committed_len[s] = keep;
       a.carry_len[s] = 0;
       if (a.carry_hist) for (int j = 0; j < a.hist_len; ++j) a.carry_hist[static_cast<size_t>(s) * a.hist_len + j] = 0;

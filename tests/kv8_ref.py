@@ -146,7 +146,7 @@ class Tables:
             for j in range(first, self.held[s]):
                 self.table[s][j] = -1
             self.held[s] = first
-            if k < self.lens[s]:
+            if k < self.lens[s] or (keep is not None and k == 0):
                 self.lens[s] = k
                 self.carry_len[s] = 0
         self.free += gone[::-1]

@@ -6,9 +6,15 @@ import pytest
 import torch
 
 from tests import kv8_ref as ref
+from tests.helpers import small_bf16
 from tests.test_kv8_gpu import _B, _check_bytes, _ctx, _i32, _values
 
 pytestmark = pytest.mark.gpu
+
+
+def H_():
+    from tests import gpu_harness
+    return gpu_harness
 
 
 # ----------------------------------------------------------------------------- set-up
@@ -194,3 +200,54 @@ def test_a_free_list_of_an_impossible_length_is_left_alone(n_free):
     for k, v in _all_of(st, pages).items():
         assert torch.equal(v, was[k]), k
     ctx.close()
+
+
+def test_a_request_that_ends_without_tokens_leaves_no_carried_rows():
+    """keep = 0 ends a request at any length, 0 included; a release without keep does not, whatever the length."""
+    ctx, st, cfg, pages, t = _held_state(lens=(0, 33, 0, 40))
+    ctx.pages_release(pages, None, st, 4)
+    assert st.carry_len.tolist() == [3, 3, 3, 3] and st.carry_hist.tolist() == [[1, 1]] * 4
+    ctx.pages_release(pages, _i32([0, 33, 5, 0]), st, 4)
+    assert st.committed_len.tolist() == [0, 33, 0, 0]
+    assert st.carry_len.tolist() == [0, 3, 3, 0] and st.carry_hist.tolist() == [[0, 0], [1, 1], [1, 1], [0, 0]]
+    assert ctx.poll_status() == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("carry_rounds", [1, 2])
+def test_the_next_request_in_a_place_does_not_see_the_last_one_s_rows(carry_rounds):
+    """An empty request whose window was rejected whole ends; a new one with the same window in its place drafts what a fresh
+    state drafts."""
+    B = _B()
+    wl = small_bf16(S=2, W=8, n_layers=1, ctx=(0, 0), kv8=True, n_rounds=6, carry_rounds=carry_rounds)
+    pair = H_().Pair(wl, 6, fill_pool=False)
+    st, ctx = pair.st_g, pair.ctx
+    pages = B.Pages(pair.cfg_g, 2)
+    rd, dev = pair.round_inputs(0)
+    other = dev["draft"].clone()
+    other[:] = (dev["target"][:, :8] + 1) % wl.shape.vocab       # nothing is accepted
+    fresh = [x.clone() for x in (st.kv_pool.view(torch.uint8), st.kv_scale, st.carry_kv)]
+
+    def rounds():
+        seen = []
+        for draft in (other, dev["draft"]):
+            ctx.pages_reserve(pages, _i32([8, 8]), st, 2)
+            ctx.draft_round(draft, dev["target"], dev["H"], 2, 0, B.COD_CARRY, st, pair.split, pair.next_draft, pair.taps)
+            ctx.pages_release(pages, None, st, 2)
+            seen += [pair.taps.x_final.clone(), st.carry_len.clone()]
+        return seen
+
+    st.block_table.fill_(-1)
+    st.committed_len.zero_()
+    want = rounds()
+    ctx.pages_release(pages, _i32([0, 0]), st, 2)
+    ctx.pages_reserve(pages, _i32([8, 8]), st, 2)
+    ctx.draft_round(other, dev["target"], dev["H"].flip(0).contiguous(), 2, 0, B.COD_CARRY, st, pair.split, pair.next_draft, pair.taps)
+    assert st.committed_len.tolist() == [0, 0] and (st.carry_len == 8).all()
+    ctx.pages_release(pages, _i32([0, 0]), st, 2)                # the request ends; the places are taken again
+    for x, y in zip((st.kv_pool.view(torch.uint8), st.kv_scale, st.carry_kv), fresh):
+        x.copy_(y)
+    got = rounds()
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert ctx.poll_status() == 0
+    pair.close()
