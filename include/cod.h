@@ -100,8 +100,9 @@ enum cod_mode {
 
 /* bits of the sticky device status word */
 #define COD_DEV_BAD_TOKEN 1u      /* a token id outside [0, vocab) was met (treated as id 0) */
-#define COD_DEV_PAGE_OVERFLOW 2u  /* a position fell beyond max_pages_per_seq (row not stored) */
-#define COD_DEV_BAD_PAGE 4u       /* block_table held a page id outside [0, n_pages) */
+#define COD_DEV_PAGE_OVERFLOW 2u  /* a position fell beyond max_pages_per_seq (the sequence sits the round out) */
+#define COD_DEV_BAD_PAGE 4u       /* block_table held a page id outside [0, n_pages); where an accepted row was to go there,
+                                     the sequence sits the round out */
 #define COD_DEV_TIMEOUT 8u        /* a bounded device-side wait gave up */
 #define COD_DEV_BAD_LEN 16u       /* committed_len / carry_len outside its range; a negative n_new or keep; held or n_free outside its range */
 #define COD_DEV_NO_PAGES 32u      /* cod_pages_reserve: the free list ran out, at least one sequence got nothing */
@@ -190,11 +191,11 @@ typedef struct {
 
 /* Output of cod_verify_accept (device, caller-owned). Row ids are s*W + p. */
 typedef struct {
-  int32_t* accept_len;  /* [S]     m_s                                                      */
-  int32_t* bonus;       /* [S]     target[s, m_s]                                           */
+  int32_t* accept_len;  /* [S]     m_s (0 for a sequence that sits the round out)           */
+  int32_t* bonus;       /* [S]     target[s, m_s] (draft[s, 0] for one that sits out; without a draft, at temperature 1, -1) */
   int32_t* row_pos;     /* [S*W]   absolute position L_s + p                                */
   int32_t* commit_slot; /* [S*W]   page*page_size + offset for accepted rows, else -1       */
-  int32_t* carry_slot;  /* [S*W]   s*W + (p - m_s) for rejected rows, else -1               */
+  int32_t* carry_slot;  /* [S*W]   s*W + (p - m_s) for rejected rows, else -1; -1 for all rows of a sequence that sits out */
   int32_t* acc_rows;    /* [S*W]   accepted row ids, increasing; tail filled with -1        */
   int32_t* acc_off;     /* [S+1]   exclusive prefix sums of m_s                             */
   int32_t* rej_rows;    /* [S*W]   rejected row ids, increasing; tail filled with -1        */
@@ -231,7 +232,11 @@ int cod_set_weights(cod_ctx* ctx, const cod_weights* w, cod_stream_t stream);
    target [S, W+1] device int32: the target's greedy token for each window row, so
                    target[s, m_s] is the bonus token.
    m_s = longest prefix with draft == target, the first n_forced (0 or 1) rows always
-   accepted. Reads st->committed_len and st->block_table; modifies no state. */
+   accepted. Reads st->committed_len and st->block_table; modifies no state.
+   A sequence with an accepted row for which block_table has no page (cod_pages_reserve refused it, say) sits the round out:
+   accept_len 0 and no row with a slot, COD_DEV_BAD_PAGE or COD_DEV_PAGE_OVERFLOW. Parts 3 to 5 then leave its cache, its carried
+   rows and its lengths as they are and draft from draft[s, 0], i.e. the present window again: the caller presents the same
+   window in a later round. */
 int cod_verify_accept(cod_ctx* ctx, const int32_t* draft, const int32_t* target, int S,
                       int n_forced, const cod_state* st, cod_split* out, cod_stream_t stream);
 
@@ -282,8 +287,8 @@ int cod_kv_append(cod_ctx* ctx, const void* J, const int32_t* slot, int n_rows, 
      need[s] = max(0, ceil((committed_len[s] + n_new[s]) / page_size) - held[s]) pages.
    Sequences are served in order while the free list lasts: s is served if need[s] = 0 or need[0] + .. + need[s] <=
    n_free. The page of rank r among those handed out is free_list[n_free - 1 - r], ranks counted by sequence, then by
-   position in the table. Served sequences get their table entries and held[s] grows; a refused one is left as it was
-   (COD_DEV_NO_PAGES; COD_DEV_PAGE_OVERFLOW where the length does not fit max_pages_per_seq, which needs no pages).
+   position in the table. Served sequences get their table entries and held[s] grows; a refused one is left as it was, and
+   rounds leave it so while an accepted row of it has no page (cod_verify_accept) (COD_DEV_NO_PAGES; COD_DEV_PAGE_OVERFLOW where the length does not fit max_pages_per_seq, which needs no pages).
    n_new [S] device int32 (>= 0). plan (host struct, may be NULL): where the new rows go. advance != 0: committed_len[s]
    += n_new[s] for the served sequences, for callers that append those rows next.
    release: sequence s keeps its first keep[s] tokens: pages held beyond ceil(keep[s] / page_size) go back onto the free

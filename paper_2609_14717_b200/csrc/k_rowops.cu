@@ -163,7 +163,7 @@ __global__ void k_kv_finish(const float* __restrict__ part, int splits, int n_ro
   const int i = blockIdx.x, l = blockIdx.y;
   if (i >= (dense_base ? (*n_rows_dev > 0 ? n_rows : 0) : valid_rows(n_rows_dev, n_rows))) return;
   const int row = a_rows ? a_rows[i] : i;
-  if (dense_base && carry_slot[row] >= 0) return;   // the baseline drafter keeps no rejected row
+  if (dense_base && commit_slot[row] < 0) return;   // the baseline drafter keeps accepted rows only
   const int kvw = n_kv * hd, half = hd >> 1, ldc = 2 * Ld * kvw;
   const float* cs = rope_win + static_cast<size_t>(row) * hd;
 
@@ -299,9 +299,14 @@ __global__ void k_store_rows(const T* __restrict__ J, int n_rows, int n_kv, int 
   }
 }
 
+// A sequence that sits the round out (an accepted row of it had no page): none of its rows is accepted and none is carried.
+__device__ __forceinline__ bool cod_sits_out(const int* accept_len, const int* carry_slot, int s, int W) {
+  return accept_len[s] == 0 && carry_slot[static_cast<size_t>(s) * W] < 0;
+}
 // committed_len[s] += m_s; carry_len[s] = kept rows + W - m_s (0 for the baseline drafter)
 struct LensUpdate {
   const int* accept_len;      // null: no update
+  const int* carry_slot;
   int S, W, mode, max_tokens;
   int* committed_len;
   int* carry_len;
@@ -309,6 +314,7 @@ struct LensUpdate {
   const int* carry_base;
 };
 __device__ __forceinline__ void cod_update_lens_one(const LensUpdate& u, int s) {
+  if (cod_sits_out(u.accept_len, u.carry_slot, s, u.W)) return;
   const int m = u.accept_len[s];
   const int L = u.committed_len[s] + m;
   if (L > u.max_tokens) atomicOr(u.status, COD_DEV_PAGE_OVERFLOW);
@@ -325,12 +331,13 @@ __global__ void k_update_lens(LensUpdate u) {
 // Per sequence: the oldest of the k retained rounds leaves U. hist[s][0..k) holds the segment lengths,
 // oldest first (zeros at the start: empty rounds). base[s] = rows that stay; the history shifts and
 // takes the new round's W - m. The baseline drafter keeps no U: history and base are cleared.
-__global__ void k_carry_age_hist(const int* __restrict__ accept_len, const int* __restrict__ carry_len, int S, int W,
-                                 int k, int mode, int* __restrict__ hist, int* __restrict__ base, int* __restrict__ drop) {
+__global__ void k_carry_age_hist(const int* __restrict__ accept_len, const int* __restrict__ carry_slot,
+                                 const int* __restrict__ carry_len, int S, int W, int k, int mode, int* __restrict__ hist, int* __restrict__ base, int* __restrict__ drop) {
   cod_pdl_prologue();
   const int s = blockIdx.x * blockDim.x + threadIdx.x;
   if (s >= S) return;
   int* h = hist + static_cast<size_t>(s) * k;
+  if (cod_sits_out(accept_len, carry_slot, s, W)) { base[s] = 0; drop[s] = 0; return; }   // nothing moves
   if (mode != COD_CARRY) {
     for (int j = 0; j < k; ++j) h[j] = 0;
     base[s] = 0; drop[s] = 0;
@@ -707,7 +714,7 @@ int cod_launch_store_rows(cod_ctx* c, const void* J, const int32_t* slot, int n_
 
 int cod_launch_update_lens(cod_ctx* c, const cod_split* sp, int S, int mode, const cod_state* ds, cudaStream_t st) {
   ProfScope prof(c, COD_K_ROWOPS, st);
-  const LensUpdate u{sp->accept_len, S, c->cfg.block, mode, c->cfg.max_pages_per_seq * c->cfg.page_size,
+  const LensUpdate u{sp->accept_len, sp->carry_slot, S, c->cfg.block, mode, c->cfg.max_pages_per_seq * c->cfg.page_size,
                      ds->committed_len, ds->carry_len, c->status, c->carry_base};
   cod_launch_pdl(c, k_update_lens, (S + 127) / 128, 128, 0, st, u);
   COD_CHECK_LAUNCH(c);
@@ -718,7 +725,7 @@ int cod_launch_carry_age(cod_ctx* c, const cod_split* sp, int S, int mode, const
   ProfScope prof(c, COD_K_ROWOPS, st);
   const cod_config& f = c->cfg;
   const int k = c->carry_cap / f.block;
-  cod_launch_pdl(c, k_carry_age_hist, (S + 127) / 128, 128, 0, st, sp->accept_len, ds->carry_len, S, f.block, k, mode,
+  cod_launch_pdl(c, k_carry_age_hist, (S + 127) / 128, 128, 0, st, sp->accept_len, sp->carry_slot, ds->carry_len, S, f.block, k, mode,
                  ds->carry_hist, c->carry_base, c->carry_drop);
   COD_CHECK_LAUNCH(c);
   const dim3 grid(S, f.n_kv_heads * 2, f.n_layers);
@@ -735,7 +742,7 @@ int cod_launch_embed_norm(cod_ctx* c, const int32_t* bonus, int S, cudaStream_t 
   const cod_config& f = c->cfg;
   const int R = S * f.block;
   LensUpdate u{};                                   // sp == null: no length update rides along
-  if (sp) u = LensUpdate{sp->accept_len, S, f.block, mode, f.max_pages_per_seq * f.page_size, ds->committed_len,
+  if (sp) u = LensUpdate{sp->accept_len, sp->carry_slot, S, f.block, mode, f.max_pages_per_seq * f.page_size, ds->committed_len,
                          ds->carry_len, c->status, c->carry_base};
   if (row_narrow(c->D)) {
     DISPATCH_T(c,

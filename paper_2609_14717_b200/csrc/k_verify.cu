@@ -56,11 +56,20 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
   uint32_t flags = 0;
 
   for (int s = wid; s < S; s += nw) {
+    const int L = committed_len[s];
     int m = W;
+    uint32_t missing = 0;                     // why an accepted row has no place, if one has none
     for (int p0 = 0; p0 < W && m == W; p0 += 32) {
       const int p = p0 + lane;
       bool ok = true;
+      uint32_t no_place = 0;
       if (p < W) {
+        const int lp = L < 0 || L > 0x7FFFFFFF - W ? max_pages : (L + p) / page;
+        if (lp >= max_pages) no_place = COD_DEV_PAGE_OVERFLOW;
+        else {
+          const int pg = block_table[static_cast<size_t>(s) * max_pages + lp];
+          if (pg < 0 || pg >= n_pages) no_place = COD_DEV_BAD_PAGE;
+        }
         if (p_tok == nullptr) {                       // greedy: the drafted token is the target's token
           const int d = draft[s * W + p], t = target[s * (W + 1) + p];
           if (d < 0 || d >= vocab || t < 0 || t >= vocab) flags |= COD_DEV_BAD_TOKEN;
@@ -71,12 +80,17 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
       }
       const unsigned miss = __ballot_sync(0xffffffffu, !ok);
       if (miss) m = p0 + __ffs(miss) - 1;
+      missing |= __reduce_or_sync(0xffffffffu, p < m ? no_place : 0u);
     }
     if (lane == 0) {
-      s_m[s] = m;
-      int b = target[s * (W + 1) + m];
-      if (b < 0 || b >= vocab) { flags |= COD_DEV_BAD_TOKEN; b = 0; }
-      out.accept_len[s] = m;
+      // an accepted row without a page (cod_pages_reserve refused the sequence): it sits this round out and nothing of it changes.
+      // Its next block is drafted from its window's first token, i.e. it is the present one again.
+      const bool waits = missing != 0;
+      flags |= missing;
+      s_m[s] = waits ? -1 : m;
+      int b = !waits ? target[s * (W + 1) + m] : draft != nullptr ? draft[s * W] : -1;
+      if ((b < 0 || b >= vocab) && (!waits || draft != nullptr)) { flags |= COD_DEV_BAD_TOKEN; b = 0; }
+      out.accept_len[s] = waits ? 0 : m;
       out.bonus[s] = b;
     }
   }
@@ -87,7 +101,7 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
     int run = 0;
     for (int s0 = 0; s0 < S; s0 += 32) {
       const int s = s0 + lane;
-      const int v = s < S ? s_m[s] : 0;
+      const int v = s < S ? max(s_m[s], 0) : 0;
       int inc = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -107,24 +121,17 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
   }
   const int R = S * W, acc_total = s_acc[S];
   for (int r = threadIdx.x; r < R; r += blockDim.x) {
-    const int s = r / W, p = r - s * W, m = s_m[s];
+    const int s = r / W, p = r - s * W, m = max(s_m[s], 0);
     const int L = committed_len[s];
     if (L < 0) flags |= COD_DEV_BAD_LEN;
     const int pos = L + p;
     out.row_pos[r] = pos;
     int cslot = -1, uslot = -1;
     if (p < m) {
-      const int lp = pos / page;
-      if (L < 0 || lp >= max_pages) {
-        flags |= COD_DEV_PAGE_OVERFLOW;
-      } else {
-        const int pg = block_table[s * max_pages + lp];
-        if (pg < 0 || pg >= n_pages) flags |= COD_DEV_BAD_PAGE;
-        else cslot = pg * page + pos % page;
-      }
+      cslot = block_table[static_cast<size_t>(s) * max_pages + pos / page] * page + pos % page;
       out.acc_rows[s_acc[s] + p] = r;
     } else {
-      uslot = s * W + (p - m);
+      if (s_m[s] >= 0) uslot = s * W + (p - m);
       out.rej_rows[(s * W - s_acc[s]) + (p - m)] = r;
     }
     out.commit_slot[r] = cslot;
@@ -137,7 +144,7 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
     for (int e = threadIdx.x; e < R * tabs.half; e += blockDim.x) {
       const int r = e / tabs.half, j = e - r * tabs.half, s = r / W, p = r - s * W;
       const int L = max(committed_len[s], 0);
-      rope_entry(tabs, r, j, L + p, L + s_m[s] + p);
+      rope_entry(tabs, r, j, L + p, L + max(s_m[s], 0) + p);
     }
 }
 

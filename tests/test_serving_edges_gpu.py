@@ -251,3 +251,145 @@ def test_the_next_request_in_a_place_does_not_see_the_last_one_s_rows(carry_roun
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert ctx.poll_status() == 0
     pair.close()
+
+
+# ----------------------------------------------------------------------------- rounds without pages
+def _serve(kv8, mode, carry_rounds, starve, n_inputs=6, S=3, W=8):
+    """Prompts, then one captured step (trim, reserve, round) replayed until every sequence has been through n_inputs windows. In the
+    replays that `starve` names nothing is on the free list. Returns the state and what each window of each sequence gave."""
+    B, H = _B(), H_()
+    wl = small_bf16(S=S, W=W, n_layers=2, ctx=(1, 60), kv8=kv8, n_rounds=16, carry_rounds=carry_rounds)
+    pair = H.Pair(wl, 4, fill_pool=False)
+    sh, st, ctx = wl.shape, pair.st_g, pair.ctx
+    st.block_table.fill_(-1)
+    st.committed_len.zero_()
+    pages, prompts = B.Pages(pair.cfg_g, S), [37, 0, 50]
+    plan = B.RowPlan(S, sum(prompts))
+    ctx.pages_reserve(pages, _i32(prompts), st, S, plan, advance=True)
+    J = torch.from_numpy(np.random.default_rng(8).normal(size=(2, plan.max_rows, 2, sh.n_kv, 128))).to(torch.bfloat16).cuda()
+    ctx.kv_append(J, plan.slot, st)
+    room = torch.full((S,), W, dtype=torch.int32, device="cuda")
+    inputs = [pair.round_inputs(r)[1] for r in range(n_inputs)]
+    dev = {k: v.clone() for k, v in inputs[0].items()}
+
+    def step():
+        ctx.pages_release(pages, None, st, S)
+        ctx.pages_reserve(pages, room, st, S)
+        ctx.draft_round(dev["draft"], dev["target"], dev["H"], S, 1, mode, st, pair.split, pair.next_draft, pair.taps)
+
+    tensors = [t for t in (st.kv_pool.view(torch.uint8), st.kv_scale, st.committed_len, st.carry_kv, st.carry_len, st.carry_hist, st.block_table,
+                           pages.free_list, pages.n_free, pages.held) if t is not None]
+    saved = [t.clone() for t in tensors]
+    step()                                                     # warm-up, taken back
+    for t, x in zip(tensors, saved):
+        t.copy_(x)
+    ctx.poll_status()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    at, gave, sat_out, r = [0] * S, [[] for _ in range(S)], 0, 0
+    while min(at) < n_inputs:
+        for k, v in dev.items():
+            rows = v.shape[0] // S
+            for s in range(S):
+                v[s * rows:(s + 1) * rows] = inputs[min(at[s], n_inputs - 1)][k][s * rows:(s + 1) * rows]
+        hog = []
+        if r in starve:
+            ctx.pages_release(pages, None, st, S)
+            hog = pages.free_list[:int(pages.n_free)].tolist()
+            pages.n_free.zero_()
+        before = [t.clone() for t in (st.committed_len, st.carry_len, st.carry_kv)] + [st.carry_hist.clone() if st.carry_hist is not None else None]
+        mine = [_rows_of(st, s) for s in range(S)]
+        g.replay()
+        torch.cuda.synchronize()
+        flags, m, slots = ctx.poll_status(), pair.split.accept_len.tolist(), pair.split.carry_slot.view(S, W)
+        want_flags = 0
+        for s in range(S):
+            if at[s] >= n_inputs:                              # (a sequence that is through goes on with its last window; it is not looked at)
+                want_flags |= flags & (B.DEV_BAD_PAGE | B.DEV_NO_PAGES)
+                continue
+            if m[s] == 0:                                      # (with a forced first row a round that goes ahead accepts one at least)
+                assert r in starve and (slots[s] == -1).all()
+                sat_out += 1
+                want_flags |= B.DEV_BAD_PAGE
+                assert int(pair.split.bonus[s]) == int(dev["draft"][s, 0]) == int(pair.next_draft[s, 0])
+                for x, y in zip((st.committed_len, st.carry_len), before):
+                    assert torch.equal(x[s], y[s])
+                assert torch.equal(st.carry_kv[:, s], before[2][:, s]) and (before[3] is None or torch.equal(st.carry_hist[s], before[3][s]))
+                assert all(torch.equal(x, y) for x, y in zip(_rows_of(st, s), mine[s]))
+                continue
+            gave[s].append((m[s], int(pair.split.bonus[s]), int(st.committed_len[s]), int(st.carry_len[s]),
+                            st.carry_kv[:, s, :, :, :int(st.carry_len[s])].clone(), pair.taps.x_final.view(S, W, -1)[s].cpu().numpy()))
+            at[s] += 1
+        assert flags & ~B.DEV_NO_PAGES == want_flags & ~B.DEV_NO_PAGES and (not want_flags or flags & B.DEV_NO_PAGES)
+        if hog:                                                # the pages come back, below those that are free by now
+            now = hog + pages.free_list[:int(pages.n_free)].tolist()
+            pages.free_list[:len(now)] = _i32(now)
+            pages.n_free.fill_(len(now))
+        r += 1
+        assert r < 40
+    del g
+    final = [_rows_of(st, s, gave[s][-1][2]) for s in range(S)]
+    pair.close()
+    return gave, final, sat_out
+
+
+def _rows_of(st, s, L=None):
+    """The bits of a sequence's committed rows, [Ld, n_kv, 2, L, hd], and its pages' scales."""
+    L = int(st.committed_len[s]) if L is None else L
+    ids = st.block_table[s, :(L + 15) // 16].long()
+    bits = st.kv_pool.view(torch.uint8 if st.kv_scale is not None else torch.int16)[:, ids]        # [Ld, pages, n_kv, 2, 16, hd]
+    rows = bits.permute(0, 2, 3, 1, 4, 5).flatten(3, 4)[:, :, :, :L]
+    return rows.clone(), st.kv_scale[:, ids].clone() if st.kv_scale is not None else torch.zeros(0)
+
+
+@pytest.mark.parametrize("kv8,mode,carry_rounds", [(True, 0, 1), (True, 0, 2), (True, 1, 1), (False, 0, 1)])
+def test_a_sequence_without_pages_waits_and_goes_on_as_if_nothing_had_been(kv8, mode, carry_rounds):
+    """The free list runs out inside the captured loop, then pages come back: the sequences that had to wait lose nothing."""
+    from tests.helpers import rel_err
+    gave, final, waited = _serve(kv8, mode, carry_rounds, starve=range(1, 6))
+    want, end, none = _serve(kv8, mode, carry_rounds, starve=())
+    assert waited >= 6 and none == 0
+    for s in range(3):
+        for i, (x, y) in enumerate(zip(gave[s][:6], want[s][:6])):
+            assert x[:4] == y[:4] and torch.equal(x[4], y[4]), (s, i)
+            assert rel_err(x[5], y[5]) < H_().TOL["bf16"], (s, i)
+        L = want[s][5][2]
+        assert gave[s][5][2] == L
+        if kv8:                                                # whole pages: a sequence that was through first has gone on in its last one
+            assert torch.equal(final[s][1][:, :L // 16], end[s][1][:, :L // 16])
+            L = L // 16 * 16
+        assert torch.equal(final[s][0][:, :, :, :L], end[s][0][:, :, :, :L])
+
+
+def test_a_round_at_temperature_1_leaves_a_sequence_without_pages_alone():
+    """The same in one eager round of the stochastic form and through the parts; a sequence beyond its table's end waits, too."""
+    B, H = _B(), H_()
+    wl = small_bf16(S=3, W=16, n_layers=1, ctx=(40, 60), kv8=True, n_rounds=4)
+    pair = H.Pair(wl, 3, fill_pool=False)
+    st, ctx, S, W = pair.st_g, pair.ctx, 3, 16
+    rd, dev = pair.round_inputs(0)
+    st.committed_len.copy_(_i32([47, 47, pair.cfg_g.max_pages_per_seq * 16 - 3]))
+    st.block_table[1, 3:] = -1
+    st.carry_len.fill_(5)
+    ones, zeros = torch.ones((S, W), device="cuda"), torch.zeros((S, W), device="cuda")
+    was = [t.clone() for t in (st.kv_pool.view(torch.uint8), st.kv_scale, st.carry_kv)]
+    ctx.draft_round_stochastic(dev["target"], ones, ones, zeros, dev["H"], S, 1, B.COD_CARRY, st, pair.split, pair.next_draft, pair.taps)
+    assert ctx.poll_status() == B.DEV_BAD_PAGE | B.DEV_PAGE_OVERFLOW
+    assert pair.split.accept_len.tolist() == [16, 0, 0] and pair.split.bonus.tolist()[1:] == [-1, -1] == pair.next_draft[1:, 0].tolist()
+    assert pair.split.acc_off.tolist() == [0, 16, 16, 16] and pair.split.rej_off.tolist() == [0, 0, 16, 32]
+    assert pair.split.rej_rows.tolist() == list(range(16, 48)) + [-1] * 16 and pair.split.acc_rows.tolist() == list(range(16)) + [-1] * 32
+    assert st.committed_len.tolist() == [63, 47, pair.cfg_g.max_pages_per_seq * 16 - 3] and st.carry_len.tolist() == [0, 5, 5]
+    changed = [int(p) for p in (st.kv_scale != was[1]).flatten(2).any(-1).any(0).nonzero().flatten()]
+    assert set(changed) <= set(st.block_table[0, :4].tolist()) and torch.equal(st.carry_kv, was[2])
+    # by parts: rows 0 and 1 of a window that fits are accepted, the others carried
+    draft = dev["draft"].clone()
+    draft[:, 2] = (dev["target"][:, 2] + 1) % wl.shape.vocab
+    draft[:, 1] = dev["target"][:, 1]
+    ctx.verify_accept(draft, dev["target"], S, 1, st, pair.split)
+    assert pair.split.accept_len.tolist() == [2, 0, 2] and pair.split.bonus[1] == draft[1, 0]
+    J = torch.ones((1, S * W, 2, wl.shape.n_kv, 128), dtype=torch.bfloat16, device="cuda")
+    ctx.scatter_kv(J, pair.split, S, B.COD_CARRY, st)
+    assert st.committed_len.tolist() == [65, 47, pair.cfg_g.max_pages_per_seq * 16 - 1] and st.carry_len.tolist() == [14, 5, 14]
+    assert torch.equal(st.carry_kv[:, 1], was[2][:, 1]) and ctx.poll_status() == B.DEV_BAD_PAGE
+    pair.close()
