@@ -1,0 +1,117 @@
+"""Attention over the 8-bit cache against its error model: rows and carried shares within what the roundings explain, so that a
+lost key, a wrong scale or a share that is not computed shows. The checks themselves are tested on the host."""
+import numpy as np
+import pytest
+import torch
+
+from tests import kv8_model as model
+from tests import kv8_ref as ref
+
+
+def _bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).double().numpy()
+
+
+def _host_case(S=2, W=4, n_q=4, n_kv=2, hd=64, lens=(900, 33), seed=0):
+    rng = np.random.default_rng(seed)
+    n = [(L + 15) // 16 for L in lens]
+    x = rng.normal(size=(sum(n), n_kv, 2, 16, hd)) * 2.0 ** rng.integers(-1, 2, size=(sum(n), n_kv, 2, 1, 1))
+    scale = np.vectorize(ref.scale_for)(np.abs(x).max((-1, -2)))
+    pool = ref.e4m3(x / scale[..., None, None])
+    table = np.full((S, max(n) + 1), -1)
+    order = rng.permutation(sum(n))
+    for s in range(S):
+        table[s, :n[s]] = order[sum(n[:s]):sum(n[:s + 1])]
+    mk = lambda *sh: _bf16(rng.normal(size=sh))  # noqa: E731
+    return dict(q=mk(S, W, n_q, hd), kb=mk(S, W, n_kv, hd), vb=mk(S, W, n_kv, hd), pool=pool, scale=scale, table=table, lens=list(lens),
+                carry=mk(S, n_kv, 2, W, hd), carry_len=[W, 1], theta=1e6)
+
+
+def test_the_model_accepts_what_rounded_arithmetic_gives():
+    """Rotated q and block keys rounded to bf16, output to bf16."""
+    for seed in range(3):
+        c = _host_case(seed=seed)
+        want = model.attend(**c)
+        pos = (np.array(c["lens"])[:, None] + np.arange(4))[:, :, None]
+        turn = lambda x: ref.rope(_bf16(ref.rope(x, pos, 1e6)), -pos, 1e6)  # noqa: E731
+        got = model.attend(**(c | {"q": turn(c["q"]), "kb": turn(c["kb"])}))
+        model.check(_bf16(got[0]), want[0], want[1], got[2], want[2], want[3])
+
+
+@pytest.mark.parametrize("what", ["zero", "mass_zero", "mass_twice", "lost_key", "scale_k", "scale_v", "rows_swapped", "no_carry", "one_more_token"])
+def test_the_checks_refuse_wrong_results(what):
+    c = _host_case()
+    want = model.attend(**c)
+    out, mass = want[0], want[2]
+    first = int(c["table"][0, 7])
+    if what == "zero":
+        out = 0 * out
+    elif what == "mass_zero":
+        mass = 0 * mass
+    elif what == "mass_twice":
+        mass = 2 * mass
+    elif what == "lost_key":                                    # one of 900
+        out = model.attend(**c, drop={(0, 0): 415})[0]
+    elif what.startswith("scale"):                              # of one page of 57, one head
+        c["scale"] = c["scale"].copy()
+        c["scale"][first, 0, int(what == "scale_v")] *= 2
+        out = model.attend(**c)[0]
+    elif what == "rows_swapped":
+        out = out[:, :, [1, 0, 2, 3]]
+    elif what == "no_carry":
+        out = model.attend(**(c | {"carry_len": [0, 0]}))[0]
+    elif what == "one_more_token":
+        out = model.attend(**(c | {"lens": [901, 33]}))[0]
+    with pytest.raises(AssertionError):
+        model.check(_bf16(out), want[0], want[1], mass, want[2], want[3])
+
+
+# ----------------------------------------------------------------------------- the kernels
+def _gpu():
+    from tests import test_kv8_gpu
+    return test_kv8_gpu
+
+
+CASES = {
+    "token": dict(S=4, W=1, n_q=8, n_kv=2, hd=128, lens=[0, 1, 17, 900], carry=False),
+    "token_mqa": dict(S=2, W=1, n_q=16, n_kv=1, hd=128, lens=[1000, 77], carry=True),
+    "rows8": dict(S=3, W=2, n_q=8, n_kv=2, hd=128, lens=[45, 1000, 16], carry=True),
+    "rows9": dict(S=2, W=9, n_q=2, n_kv=2, hd=128, lens=[500, 31], carry=True),
+    "block16": dict(S=3, W=16, n_q=8, n_kv=2, hd=128, lens=[0, 33, 1025], carry=True),
+    "rows66": dict(S=2, W=22, n_q=6, n_kv=2, hd=128, lens=[400, 129], carry=True),
+    "block32": dict(S=2, W=32, n_q=4, n_kv=1, hd=128, lens=[7, 1100], carry=True),
+    "retained": dict(S=2, W=16, n_q=4, n_kv=1, hd=128, lens=[40, 300], carry=True, carry_rounds=4),
+    "hd64_token": dict(S=3, W=1, n_q=8, n_kv=2, hd=64, lens=[0, 65, 700], carry=True),
+    "hd64_block16": dict(S=2, W=16, n_q=8, n_kv=2, hd=64, lens=[160, 1025], carry=True),
+    # row tiles in more than one pass over the keys, the last one not full
+    "hd64_rows96": dict(S=2, W=24, n_q=8, n_kv=2, hd=64, lens=[130, 1025], carry=True),
+    "hd64_rows100": dict(S=3, W=25, n_q=8, n_kv=2, hd=64, lens=[0, 47, 600], carry=True),
+    "hd64_block32": dict(S=2, W=32, n_q=8, n_kv=2, hd=64, lens=[700, 16], carry=True),
+}
+
+
+def _run(case, flags=0, seed=1, **kw):
+    T = _gpu()
+    ctx, st, args, *_ = T._attn_case(**(CASES[case] if isinstance(case, str) else case), flags=flags, seed=seed)
+    return ctx, st, args
+
+
+def _compare(ctx, st, args):
+    T = _gpu()
+    layer, q, kb, vb, _, S, use, out, mass = args
+    v = T._values
+    ctx.block_attn(*args)
+    lens, car = st.committed_len.tolist(), [c if use else 0 for c in st.carry_len.tolist()]
+    want = model.attend(v(q), v(kb), v(vb), np.nan_to_num(v(st.kv_pool)[layer]), np.nan_to_num(v(st.kv_scale)[layer]), st.block_table.cpu().numpy(),
+                        lens, np.nan_to_num(v(st.carry_kv)[layer]), car, 1e6)
+    model.check(v(out), want[0], want[1], v(mass), want[2], want[3])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("name", CASES)
+def test_rows_are_as_near_as_their_roundings_allow(name, flags):
+    ctx, st, args = _run(name, flags)
+    _compare(ctx, st, args)
+    assert ctx.poll_status() == 0
+    ctx.close()
