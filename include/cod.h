@@ -102,7 +102,7 @@ enum cod_mode {
 #define COD_DEV_BAD_TOKEN 1u      /* a token id outside [0, vocab) was met (treated as id 0) */
 #define COD_DEV_PAGE_OVERFLOW 2u  /* a position fell beyond max_pages_per_seq (the sequence sits the round out) */
 #define COD_DEV_BAD_PAGE 4u       /* block_table held a page id outside [0, n_pages); where an accepted row was to go there,
-                                     the sequence sits the round out */
+                                     the sequence sits the round out; with COD_F_KV8 attention leaves its keys out */
 #define COD_DEV_TIMEOUT 8u        /* a bounded device-side wait gave up */
 #define COD_DEV_BAD_LEN 16u       /* committed_len / carry_len outside its range; a negative n_new or keep; held or n_free outside its range */
 #define COD_DEV_NO_PAGES 32u      /* cod_pages_reserve: the free list ran out, at least one sequence got nothing */

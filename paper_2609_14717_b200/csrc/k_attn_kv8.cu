@@ -198,7 +198,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
   int step = 0;                                             // pages this warp has been through: slot and phase of the ring
   bool ok = true;
   const uint64_t pol = l2_evict_first();
-  // K and V of a page: one box of 32 rows (page 0 in the place of a bad one) into the slot of page number `n` of this warp
+  // K and V of a page: one box of 32 rows (page 0, unused, in the place of a bad one) into the slot of page number `n` of this warp
   auto request = [&](int pg, int h, int n) {
     if (lane == 0) {
       const uint32_t bar = tc::smem_u32(full + n % STAGES);
@@ -316,13 +316,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
             for (; nx_ready < nx_nb && nb + nx_ready <= i + STAGES; ++nx_ready)
               request(__shfl_sync(0xffffffffu, nx_pg, nx_ready), nxt.h, step + nb + nx_ready);
           }
-          if (bad) {                           // reads as zeros
-#pragma unroll
-            for (int w = 0; w < CW; ++w) {
-              kr[0][0][w] = kr[0][1][w] = kr[1][0][w] = kr[1][1][w] = 0u;
-              vr[0][w] = vr[1][w] = vr[2][w] = vr[3][w] = 0u;
-            }
-          }
+          if (bad) continue;                   // its keys do not count (all lanes agree)
           float sv[NR][4], sw[NR][4];          // two chains of dependent MMAs
 #pragma unroll
           for (int n = 0; n < NR; ++n)
@@ -480,7 +474,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
   if (c < 0 || c > p.cap) { flags |= COD_DEV_BAD_LEN; c = max(0, min(c, p.cap)); }
   const int n_tail = Lr + c + p.W;
   size_t u_last = 0;                         // the partial page's K of this head
-  bool have_last = false;
+  bool have_last = false;                    // false with Lr > 0: a bad page, its keys do not count
   float2 sc = make_float2(0.f, 0.f);
   if (Lr > 0) {
     const int pg = p.block_table[static_cast<size_t>(s) * p.max_pages + L / PAGE];
@@ -582,7 +576,10 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
                 mma_bf16(sv[0], a0[2 * w], a1[2 * w], a0[2 * w + 1], a1[2 * w + 1], qc[hf * CW + w][0], qc[hf * CW + w][1]);
           }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sv[0][e] = z0 + g + (e >> 1) * 8 < nf ? sv[0][e] * sl2 : -INFINITY;
+          for (int e = 0; e < 4; ++e) {        // (the tail's first 16 keys hold one that counts: Lr < 16, and the block's own follow)
+            const int zz = z0 + g + (e >> 1) * 8;
+            sv[0][e] = zz < nf && (have_last || f0 + zz >= Lr) ? sv[0][e] * sl2 : -INFINITY;
+          }
 #pragma unroll
           for (int e = 0; e < 2; ++e) mx[0][e] = fmaxf(sv[0][e], sv[0][2 + e]);
           st.refer(mx, mx);

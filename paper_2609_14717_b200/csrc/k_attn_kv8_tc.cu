@@ -557,7 +557,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
               const int q = tid & 127;
               const float mx = fmaxf(fmaxf(xs[q], xs[NROW + q]), fmaxf(xs[2 * NROW + q], xs[3 * NROW + q])), old = starts ? -INFINITY : -nr[q];
               const bool up = mx - old > 15.f;
-              const float to = up ? mx - 10.f : starts ? 0.f : old;  // (a first tile without a single key: any)
+              // (a first tile of bad pages alone leaves the row without a reference: the first key that counts overflows, and sets it)
+              const float to = up ? mx - 10.f : old;
               fs[q] = starts ? 0.f : up ? ex2(old - to) : 1.f;
               nr[q] = -to;
             }
@@ -611,7 +612,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
       if ((tid & 127) < NROW && tid < 2 * 128) {           // the groups' factors
         const int q = tid & 127;
         const float r0 = have_0 ? -nr_s[q] : -INFINITY, r1 = have_1 ? -nr_s[NROW + q] : -INFINITY;
-        fs[q] = ex2((grp ? r1 : r0) - fmaxf(r0, r1));
+        const float top = fmaxf(r0, r1);         // -inf: not a key in the whole segment
+        fs[q] = top == -INFINITY ? 0.f : ex2((grp ? r1 : r0) - top);
       }
       sync_workers();
       // each group writes half of the rows: it takes the other's contribution from shared memory and leaves there its own to the

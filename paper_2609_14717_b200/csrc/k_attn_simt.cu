@@ -84,16 +84,18 @@ k_attn_split(const T* __restrict__ q, const T* __restrict__ kb, const T* __restr
         const int tt = t + key;
         const T *kp = nullptr, *vp = nullptr;
         if (tt < L) {
-          int pg = block_table[s * max_pages + tt / page];
-          if (pg < 0 || pg >= n_pages) { flags |= COD_DEV_BAD_PAGE; pg = 0; }
-          if (pool8 != nullptr) {
-            const size_t u = ((static_cast<size_t>(layer) * n_pages + pg) * n_kv + h) * 2;
+          int pg = block_table[static_cast<size_t>(s) * max_pages + tt / page];
+          const bool bad = pg < 0 || pg >= n_pages;
+          if (bad) { flags |= COD_DEV_BAD_PAGE; pg = 0; }
+          const size_t u = ((static_cast<size_t>(layer) * n_pages + pg) * n_kv + h) * 2;
+          if (pool8 == nullptr) {
+            kp = pool + (u * page + tt % page) * HD;
+            vp = kp + static_cast<size_t>(page) * HD;
+          } else if (!bad) {
             const uint8_t* p8 = pool8 + (u * page + tt % page) * HD + d4;
             kv4 = ld4_e4m3(p8, kv_scale[u]);
             vv4 = ld4_e4m3(p8 + static_cast<size_t>(page) * HD, kv_scale[u + 1]);
-          } else
-          kp = pool + ((((static_cast<size_t>(layer) * n_pages + pg) * n_kv + h) * 2) * page + tt % page) * HD;
-          if (kp != nullptr) vp = kp + static_cast<size_t>(page) * HD;
+          }
         } else if (tt < L + c) {
           kp = carry + ((((static_cast<size_t>(layer) * max_batch + s) * n_kv + h) * 2) * cap + (tt - L)) * HD;
           vp = kp + static_cast<size_t>(cap) * HD;
@@ -113,7 +115,11 @@ k_attn_split(const T* __restrict__ q, const T* __restrict__ kb, const T* __restr
     }
     __syncthreads();
 
-    const bool valid = lane < n_valid;
+    bool valid = lane < n_valid;
+    if (pool8 != nullptr && valid && t + lane < L) {         // a bad page's keys do not count
+      const int pg = block_table[static_cast<size_t>(s) * max_pages + (t + lane) / page];
+      valid = pg >= 0 && pg < n_pages;
+    }
     const bool is_carry = valid && (t + lane >= L) && (t + lane < L + c);
 #pragma unroll
     for (int g = 0; g < GPW; ++g) {
@@ -133,7 +139,7 @@ k_attn_split(const T* __restrict__ q, const T* __restrict__ kb, const T* __restr
         const float sv = valid ? sc[r] : -INFINITY;
         const float m_new = fmaxf(m_run[g][r], cod_warp_max(sv));
         p[r] = valid ? __expf(sv - m_new) : 0.f;
-        const float corr = __expf(m_run[g][r] - m_new);     // exp(-inf) = 0 on the first chunk
+        const float corr = m_run[g][r] == m_new ? 1.f : __expf(m_run[g][r] - m_new);   // exp(-inf) = 0 on the first chunk with a key
         l_run[g][r] = l_run[g][r] * corr + cod_warp_sum(p[r]);
         lc_run[g][r] = lc_run[g][r] * corr + cod_warp_sum(is_carry ? p[r] : 0.f);
         m_run[g][r] = m_new;

@@ -115,3 +115,54 @@ def test_rows_are_as_near_as_their_roundings_allow(name, flags):
     _compare(ctx, st, args)
     assert ctx.poll_status() == 0
     ctx.close()
+
+
+BAD = {
+    "token": dict(S=3, W=1, n_q=8, n_kv=2, hd=128, lens=[500, 40, 17], carry=False),
+    "rows8": dict(S=2, W=4, n_q=4, n_kv=2, hd=128, lens=[700, 129], carry=True),
+    "block16": dict(S=3, W=16, n_q=8, n_kv=2, hd=128, lens=[900, 300, 130], carry=True),
+    "block32": dict(S=2, W=32, n_q=4, n_kv=1, hd=128, lens=[600, 700], carry=True),
+    "hd64": dict(S=2, W=16, n_q=8, n_kv=2, hd=64, lens=[300, 40], carry=True),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("which", ["some", "last", "runs", "all"])
+@pytest.mark.parametrize("name", BAD)
+def test_keys_of_a_bad_page_do_not_count(name, which, flags):
+    """The same in every kernel: whole pages, the last one, runs that fill tiles, all of them. Page 0, which belongs to somebody
+    else, is not read in their place."""
+    T = _gpu()
+    ctx, st, args = _run(BAD[name], flags, seed=3)
+    rng = np.random.default_rng(1)
+    for s, L in enumerate(st.committed_len.tolist()):
+        n = (L + 15) // 16
+        at = {"some": rng.permutation(n)[:max(1, n // 3)], "last": [n - 1], "runs": [j for j in range(n) if j // 8 % 2 == s % 2], "all": range(n)}[which]
+        for j in at:
+            st.block_table[s, int(j)] = int(rng.choice([-1, 10 ** 6, st.kv_pool.shape[1], -2 ** 31]))
+    _compare(ctx, st, args)
+    assert ctx.poll_status() in ((T._B().DEV_BAD_PAGE,) if which != "runs" else (T._B().DEV_BAD_PAGE, 0))
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("W", [1, 16, 32])
+def test_low_scores_behind_bad_pages_keep_their_weights(W, flags):
+    """Tiles of bad pages first, then keys whose scores lie some 300 log2 units below zero: nothing but their differences counts."""
+    ctx, st, args = _run(dict(S=1, W=W, n_q=4, n_kv=1, hd=128, lens=[1200], carry=False), flags, seed=5)
+    q, kb = args[1], args[2]
+    # a direction that the rotation leaves almost alone (the lowest frequencies): q has 36 there, the keys -16, block keys too
+    q[..., 60:64] = 36.0
+    kb[..., 60:64] = -16.0
+    table = st.block_table[0].long()
+    ids = table[:75]
+    st.kv_scale[0, ids] = 1.0
+    vals = st.kv_pool[0].float()
+    vals[ids] = torch.from_numpy(np.random.default_rng(2).normal(size=tuple(vals[ids].shape))).float().cuda()
+    vals[ids, :, 0, :, 60:64] = -16.0
+    st.kv_pool[0] = vals.to(torch.float8_e4m3fn)
+    st.block_table[0, :32] = -1
+    _compare(ctx, st, args)
+    ctx.close()
