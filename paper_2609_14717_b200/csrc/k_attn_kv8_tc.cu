@@ -5,8 +5,10 @@
 // while HBM delivers, and close to what the shared memory ports carry. So both products are laid out to read as little of
 // it as possible:
 //   S^T = K Q^T  M = 128 keys, K straight from the TMA ring as e4m3 (kind::f8f6f4), no conversion. Q is two e4m3 terms,
-//                q * 2^k = q1 + q2 / 16, eight significant bits as in bf16, side by side along N: one pass over K gives
-//                both parts, S = S1 + S2 / 16.
+//                q * 2^k = q1 + q2 with a k for each row, so that its largest element lies in [2^7, 2^8): eight significant
+//                bits, as in bf16, or 2^-18 of the row's largest where that is more. Both products go into one accumulator; the
+//                row's 2^-k multiplies the score, next to the K scale. (One k for all rows of the block would be 2 to 4 % faster, but
+//                then a row's precision depends on the other tokens and heads, and one that is 2^20 larger takes it all.)
 //   O^T = V^T P^T  M = 128 columns, N = rows; V converted once to f16 (exact) and P in f16, both "MN-major": the rows of
 //                their tiles are keys, as V comes from memory and as P leaves the threads, nothing is transposed.
 // One thread holds one key of a tile and all of its rows: the K scale is one factor per thread, and so is the V scale, since
@@ -48,9 +50,9 @@ constexpr uint32_t OFF_R = OFF_K + SLOTS * T_BYTES;       // [SLOTS] V as it com
 constexpr uint32_t OFF_V = OFF_R + SLOTS * T_BYTES;       // [2][two halves of the columns][128 keys][64 f16]
 constexpr uint32_t OFF_P = OFF_V + 2 * V_BYTES;            // [PBUF][128 keys][64 rows f16]
 constexpr uint32_t OFF_CTL = OFF_P + PBUF * P_BYTES;
-constexpr uint32_t SMEM = OFF_CTL + 4352 + 1024;
+constexpr uint32_t SMEM = OFF_CTL + 4608 + 1024;
 constexpr int SBUF = 3;
-constexpr uint32_t COL_S = 0, COL_O = SBUF * 128, TMEM_COLS = 512;   // S [3][128 columns], O [2][64]
+constexpr uint32_t COL_S = 0, COL_O = SBUF * NROW, TMEM_COLS = 512;   // S [3][64 columns], O [2][64]
 // setmaxnreg: the soft-max warps' budget and the others' add up to what the block is launched with (the host checks that)
 constexpr int REGS_LAUNCH = 128, REGS_SOFTMAX = 160, REGS_OTHER = 96;
 static_assert(WORKERS * REGS_SOFTMAX + (THREADS - WORKERS) * REGS_OTHER <= THREADS * REGS_LAUNCH, "setmaxnreg budgets exceed the block's registers");
@@ -117,10 +119,9 @@ __device__ __forceinline__ void tmem_ld8_nowait(uint32_t taddr, uint32_t (&v)[8]
       : "r"(taddr));
 }
 // (these two order nothing but each other and the barriers' waits: arithmetic and stores of one step may pass the next one's)
-__device__ __forceinline__ void tmem_wait_ld(uint32_t (&v)[8], uint32_t (&w)[8]) {
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&v)[8]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-                 "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]), "+r"(w[4]), "+r"(w[5]), "+r"(w[6]), "+r"(w[7]));
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]));
 }
 // two floats at a time
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -198,8 +199,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
   float* const none_s = nr_s + 2 * NROW;                             // [64] -inf: the references that a masked key sees
   float* const f_s = none_s + NROW;                                  // [2][64] factors of a change of reference
   float* const x_s = f_s + 2 * NROW;                                 // [2][4][64] maxima or sums of a group's four key quarters
-  float* const a_s = x_s + 8 * NROW;                                 // [WARPS] maxima of q, and the factor of the scores
-  float4* const page_s = reinterpret_cast<float4*>(a_s + WARPS + 8); // [SBUF][8] K scale, V scale, log2 of it; 0, 0, -inf: no page
+  float* const q_s = x_s + 8 * NROW;                                 // [64] each row's score factor: 2^-k of its q
+  float4* const page_s = reinterpret_cast<float4*>(q_s + NROW);      // [SBUF][8] K scale, V scale, log2 of it; 0, 0, -inf: no page
   int* const scan_s = reinterpret_cast<int*>(page_s + SBUF * TPAGES);       // [THREADS / 32 + 2]
   Segment* const seg_s = reinterpret_cast<Segment*>(scan_s + THREADS / 32 + 4);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -320,8 +321,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
       }
     } else if (warp == WARP_QK) {
       // ------------------------------------------------ issuer of S^T = K Q^T. The warp stays together; one lane issues
-      const uint32_t id_qk = (1u << 4) | (static_cast<uint32_t>(2 * npad >> 3) << 17) | (static_cast<uint32_t>(TILE >> 4) << 24);
-      const uint64_t q_desc = desc_kmajor_sw128(base + OFF_Q), k_desc0 = desc_kmajor_sw128(base + OFF_K);
+      const uint32_t id_qk = (1u << 4) | (static_cast<uint32_t>(npad >> 3) << 17) | (static_cast<uint32_t>(TILE >> 4) << 24);
+      const uint64_t rest = npad * HD >> 4, q_desc = desc_kmajor_sw128(base + OFF_Q), k_desc0 = desc_kmajor_sw128(base + OFF_K);
       int n = 0, seg = 0;
       bool ok = true;
       for (Segment k = first_segment(p, line, TPAGES); k.any && ok; next_segment(p, line, TPAGES, k), ++seg) {
@@ -336,7 +337,9 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
           const uint64_t k_desc = k_desc0 + slot * (T_BYTES >> 4);
           if (elect_one()) {
 #pragma unroll
-            for (int kk = 0; kk < HD / 32; ++kk) umma_e4m3(tmem + COL_S + buf * 128, k_desc + kk * 2, q_desc + kk * 2, id_qk, kk ? 1u : 0u);
+            for (int kk = 0; kk < HD / 32; ++kk) umma_e4m3(tmem + COL_S + buf * NROW, k_desc + kk * 2, q_desc + kk * 2, id_qk, kk ? 1u : 0u);
+#pragma unroll
+            for (int kk = 0; kk < HD / 32; ++kk) umma_e4m3(tmem + COL_S + buf * NROW, k_desc + kk * 2, q_desc + rest + kk * 2, id_qk, 1u);
             umma_commit(smem_u32(s_full + buf));
             umma_commit(smem_u32(k_empty + slot));
           }
@@ -412,18 +415,15 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) a = fmaxf(a, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
-        a = cod_warp_max(a);
-        if (lane == 0) a_s[warp] = a;
-        sync_workers();                        // (the table has been read, too)
-        a = 0.f;
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) a = fmaxf(a, a_s[w]);
-        // scaled by a power of two so that the block's largest lies in [2^7, 2^8)
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
+        // each row scaled by a power of two of its own so that its largest lies in [2^7, 2^8): a row's precision does not depend on
+        // the other tokens and heads of the block. A row with an infinity, which e4m3 does not have, gets no score at all.
         int E = static_cast<int>(__float_as_uint(a) >> 23) - 127;
         E = a > 0.f ? max(E, -100) : 7;
         const float up = __uint_as_float(static_cast<uint32_t>(7 - E + 127) << 23);
         if (tid == 0) *seg_s = k;                // not kept in registers through the tiles
-        if (tid == 0) a_s[WARPS] = __uint_as_float(static_cast<uint32_t>(E - 7 + 127) << 23) * sl2;
+        if (c == 0) q_s[r] = a < INFINITY ? __uint_as_float(static_cast<uint32_t>(E - 7 + 127) << 23) : __uint_as_float(0x7FFFFFFFu);
         if (r < npad) {
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) {
@@ -436,7 +436,7 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 const float x = (hf ? hi : lo)[4 * e + 2 * u] * up, y = (hf ? hi : lo)[4 * e + 2 * u + 1] * up;
                 const uint32_t q1 = __nv_cvt_float2_to_fp8x2(make_float2(x, y), __NV_SATFINITE, __NV_E4M3);
                 const float2 back = e4m3x2_to_float2(q1);
-                const uint32_t q2 = __nv_cvt_float2_to_fp8x2(make_float2((x - back.x) * 16.f, (y - back.y) * 16.f), __NV_SATFINITE, __NV_E4M3);
+                const uint32_t q2 = __nv_cvt_float2_to_fp8x2(make_float2(x - back.x, y - back.y), __NV_SATFINITE, __NV_E4M3);
                 w1[e] |= q1 << (16 * u);
                 w2[e] |= q2 << (16 * u);
               }
@@ -449,9 +449,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(q_ready));
-        sync_workers();                        // a_s[WARPS] is set
+        sync_workers();                        // q_s is set, the table has been read
       }
-      const float qfac = a_s[WARPS];
       float2 l[NROW / 2];
 #pragma unroll
       for (int e = 0; e < NROW / 2; ++e) l[e] = make_float2(0.f, 0.f);
@@ -463,9 +462,10 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         if (ok) ok = wait_asleep(smem_u32(s_full + buf), (m / SBUF) & 1, abort_flag, p.status);
         __syncwarp();
         tc_fence_after();
-        const uint32_t s_at = t_lane + COL_S + buf * 128;
+        const uint32_t s_at = t_lane + COL_S + buf * NROW;
         const float4 pg = page_s[buf * TPAGES + (key >> 4)];
-        const float kf = pg.x * qfac, kf2 = kf * 0.0625f, vs = pg.y, lv = pg.z;
+        const float kf = pg.x * sl2, vs = pg.y, lv = pg.z;
+        auto score = [&](uint32_t s, int q, float add) { return fmaf(__uint_as_float(s), q_s[q] * kf, add); };    // log2-score of row q
         const float* const ref = lv > -INFINITY ? nr : none_s;               // a masked key: 2^-inf
         const bool starts = i < 2;             // the group's first tile of the segment sets the references
         if (m >= PBUF) wait_done(m - PBUF);    // the product of the weights that had the buffer before
@@ -474,35 +474,39 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         // serve: f16 infinity if not.
         __half2 big = __half2half2(__ushort_as_half(0));
         auto weights = [&]() {
-          const float2 k1 = make_float2(kf, kf), k2 = make_float2(kf2, kf2), v2 = make_float2(vs, vs);
-          uint32_t s1[2][8], s2[2][8];
-          float4 r[2][2];
-          tmem_ld8_nowait(s_at, s1[0]);
-          tmem_ld8_nowait(s_at + npad, s2[0]);
+          const float2 k2 = make_float2(kf, kf), v2 = make_float2(vs, vs);
+          uint32_t s[2][8];
+          float4 r[2][2], f[2][2];
+          tmem_ld8_nowait(s_at, s[0]);
           r[0][0] = *reinterpret_cast<const float4*>(ref);
           r[0][1] = *reinterpret_cast<const float4*>(ref + 4);
+          f[0][0] = *reinterpret_cast<const float4*>(q_s);
+          f[0][1] = *reinterpret_cast<const float4*>(q_s + 4);
 #pragma unroll
           for (int c = 0; c < NROW; c += 8) {
-            uint32_t (&a)[8] = s1[(c >> 3) & 1], (&b)[8] = s2[(c >> 3) & 1];
+            uint32_t (&a)[8] = s[(c >> 3) & 1];
             if (c == NROW / 2 && c >= npad) {  // (rows are padded to 32 or 64)
-              tmem_wait_ld(a, b);              // what was asked for lands before its registers serve for something else
+              tmem_wait_ld(a);                 // what was asked for lands before its registers serve for something else
               break;
             }
             const float4 (&rc)[2] = r[(c >> 3) & 1];
+            const float4 (&fc)[2] = f[(c >> 3) & 1];
             float2 u[4] = {make_float2(rc[0].x, rc[0].y), make_float2(rc[0].z, rc[0].w), make_float2(rc[1].x, rc[1].y), make_float2(rc[1].z, rc[1].w)};
-            tmem_wait_ld(a, b);
+            const float2 kq[4] = {mul2(make_float2(fc[0].x, fc[0].y), k2), mul2(make_float2(fc[0].z, fc[0].w), k2),
+                                  mul2(make_float2(fc[1].x, fc[1].y), k2), mul2(make_float2(fc[1].z, fc[1].w), k2)};
+            tmem_wait_ld(a);
             if (c + 8 < NROW) {
               const int d = c + 8 == NROW / 2 ? min(c + 8, npad - 8) : c + 8;      // (behind the last row: not used)
-              tmem_ld8_nowait(s_at + d, s1[((c >> 3) + 1) & 1]);
-              tmem_ld8_nowait(s_at + npad + d, s2[((c >> 3) + 1) & 1]);
+              tmem_ld8_nowait(s_at + d, s[((c >> 3) + 1) & 1]);
               r[((c >> 3) + 1) & 1][0] = *reinterpret_cast<const float4*>(ref + d);        // (before the stores: the compiler moves no read across one)
               r[((c >> 3) + 1) & 1][1] = *reinterpret_cast<const float4*>(ref + d + 4);
+              f[((c >> 3) + 1) & 1][0] = *reinterpret_cast<const float4*>(q_s + d);
+              f[((c >> 3) + 1) & 1][1] = *reinterpret_cast<const float4*>(q_s + d + 4);
             }
             uint32_t pk[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              u[e] = fma2(make_float2(__uint_as_float(a[2 * e]), __uint_as_float(a[2 * e + 1])), k1,
-                          fma2(make_float2(__uint_as_float(b[2 * e]), __uint_as_float(b[2 * e + 1])), k2, u[e]));
+              u[e] = fma2(make_float2(__uint_as_float(a[2 * e]), __uint_as_float(a[2 * e + 1])), kq[e], u[e]);
               const float2 w = make_float2(ex2(u[e].x), ex2(u[e].y));
               l[c / 2 + e] = add2(l[c / 2 + e], w);
               const float2 y = mul2(w, v2);
@@ -522,15 +526,13 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             // than 2^100 above everything that was in it), P again
 #pragma unroll 1
             for (int c = 0; c < npad; c += 16) {
-              uint32_t s1[16], s2[16];
-              tmem_ld16_nowait(s_at + c, s1);
-              tmem_ld16_nowait(s_at + npad + c, s2);
-              tmem_wait_ld(s1);
-              tmem_wait_ld(s2);
+              uint32_t s[16];
+              tmem_ld16_nowait(s_at + c, s);
+              tmem_wait_ld(s);
               float cm = 0.f;
 #pragma unroll
               for (int e = 0; e < 16; ++e) {
-                const float m = warp_max(fmaf(__uint_as_float(s1[e]), kf, fmaf(__uint_as_float(s2[e]), kf2, lv)));
+                const float m = warp_max(score(s[e], c + e, lv));
                 cm = lane == e ? m : cm;
               }
               if (lane < 16) xs[(warp & 3) * NROW + c + lane] = cm;
@@ -539,15 +541,13 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
               for (int c = 0; c < NROW; c += 16) {
                 if (c >= npad) break;
-                uint32_t s1[16], s2[16];
-                tmem_ld16_nowait(s_at + c, s1);
-                tmem_ld16_nowait(s_at + npad + c, s2);
-                tmem_wait_ld(s1);
-                tmem_wait_ld(s2);
+                uint32_t s[16];
+                tmem_ld16_nowait(s_at + c, s);
+                tmem_wait_ld(s);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                   float& sum = e & 1 ? l[(c + e) / 2].y : l[(c + e) / 2].x;
-                  const float before = sum - ex2(fmaf(__uint_as_float(s1[e]), kf, fmaf(__uint_as_float(s2[e]), kf2, ref[c + e])));
+                  const float before = sum - ex2(score(s[e], c + e, ref[c + e]));
                   sum = fabsf(before) < INFINITY ? before : 0.f;
                 }
               }

@@ -166,3 +166,61 @@ def test_low_scores_behind_bad_pages_keep_their_weights(W, flags):
     st.block_table[0, :32] = -1
     _compare(ctx, st, args)
     ctx.close()
+
+
+# ----------------------------------------------------------------------------- rows of one head group do not touch each other
+MIXED = {
+    "token": dict(S=2, W=1, n_q=8, n_kv=1, hd=128, lens=[700, 40], carry=True),
+    "rows16": dict(S=2, W=4, n_q=8, n_kv=2, hd=128, lens=[700, 129], carry=True),
+    "block16": dict(S=2, W=16, n_q=8, n_kv=2, hd=128, lens=[1025, 40], carry=True),
+    "block32": dict(S=2, W=32, n_q=4, n_kv=1, hd=128, lens=[700, 300], carry=True),
+    "hd64": dict(S=2, W=16, n_q=8, n_kv=2, hd=64, lens=[700, 40], carry=True),
+}
+
+
+def _compare_all_but(ctx, st, args, odd):
+    """The rows for which `odd` [S, W, n_q] is false, against the model; returns the others."""
+    T = _gpu()
+    layer, q, kb, vb, _, S, use, out, mass = args
+    v = T._values
+    ctx.block_attn(*args)
+    calm = np.where(odd[..., None], 0.0, v(q))
+    want = model.attend(calm, v(kb), v(vb), np.nan_to_num(v(st.kv_pool)[layer]), np.nan_to_num(v(st.kv_scale)[layer]), st.block_table.cpu().numpy(),
+                        st.committed_len.tolist(), np.nan_to_num(v(st.carry_kv)[layer]), st.carry_len.tolist(), 1e6)
+    rest = ~odd
+    model.check(v(out)[rest], want[0][rest], want[1][rest], v(mass)[rest], want[2][rest], want[3][rest])
+    return v(out)[odd]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("k", [10, 14, 18, 24, 40])
+@pytest.mark.parametrize("name", MIXED)
+def test_a_row_s_precision_does_not_depend_on_a_larger_one(name, k, flags):
+    """One row per head group is 2^k larger than the others, the keys by as much larger as the others are smaller."""
+    case = MIXED[name]
+    ctx, st, args = _run(case, flags, seed=7)
+    q, kb = args[1], args[2]
+    odd = np.zeros(tuple(q.shape[:3]), bool)
+    odd[:, case["W"] // 2, 1::case["n_q"] // case["n_kv"]] = True
+    q[torch.from_numpy(~odd).cuda()] *= 2.0 ** -k
+    kb *= 2.0 ** k
+    st.carry_kv[:, :, :, 0] *= 2.0 ** k
+    st.kv_scale[..., 0] *= 2.0 ** k
+    _compare_all_but(ctx, st, args, odd)
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 3e38])
+@pytest.mark.parametrize("name", MIXED)
+def test_a_row_that_is_not_finite_or_huge_leaves_the_others_alone(name, value, flags):
+    case = MIXED[name]
+    ctx, st, args = _run(case, flags, seed=8)
+    odd = np.zeros(tuple(args[1].shape[:3]), bool)
+    odd[0, case["W"] // 2, 1] = True
+    args[1][0, case["W"] // 2, 1, 5] = value
+    rows = _compare_all_but(ctx, st, args, odd)
+    assert value == 3e38 or not np.isfinite(rows).any()          # what has no score has no output, in every kernel
+    ctx.close()
