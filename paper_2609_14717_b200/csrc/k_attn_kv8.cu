@@ -17,17 +17,18 @@
 //            so a lane ends up with CH contiguous columns of two rows of the output.
 // Scores are accumulated in float from f16 operands: an e4m3 byte is exact in f16, and q is scaled by a power of two per
 // row, after which bf16 q is exact, too (down to 2^-38 of the row's largest). The K scale multiplies the score; the V scale
-// enters the exponent: with x = log2-scores, P' = 2^(x + log2 s_V - r) is what multiplies the raw V bytes. The reference r
-// of a row is only moved when P' would pass 2^15, and then to give 2^10, so P' is a normal f16 number (11 bits) down to
-// 2^-24 of the largest contribution at least. The weights' sum has a reference of its own, without V's scales: a page of
-// zeros (scale 2^-100) next to pages of large values keeps its share of the sum however far the scales lie apart.
+// enters the weights: with x = log2-scores, w = 2^(x - r) is what the sum takes and P' = w 2^(log2 s_V - d) what multiplies the
+// raw V bytes. A row's r, one of its scores, is moved when a score passes it by 60 (the sum is a plain float), its d when P' would
+// pass 2^15, and then to give 2^10, so P' is a normal f16 number (11 bits) down to 2^-24 of the largest contribution at least.
+// A page of zeros (scale 2^-100) next to pages of large values keeps its share of the sum however far the scales lie apart, and
+// as x - r is exact near the largest score and d small, scores of any size lose nothing here but their own rounding.
 //
 // Work of the paged kernel: the whole pages of all (sequence, KV head) pairs lie one behind the other on a line, which is cut
 // into as many equal stretches as blocks fit on the machine at once, whatever the lengths are: one wave, no block waits for
 // a longer one, and the cost of starting up (dependent trips to memory for lengths, table, scales and the first copy) is
 // paid once per block. At a segment's end the ring already fills with the next segment's pages. The block's four warps share
 // the row tiles of the query rows and, between them, the pages; their results are joined in shared memory and leave as one
-// unnormalised partial (o, r, l, -, rl) per segment. Block i's partial of pair j is slot i + j: along the line each segment
+// unnormalised partial (o; d, r, l, -) per segment. Block i's partial of pair j is slot i + j: along the line each segment
 // moves on by a block, a pair or both, so no two meet.
 // The finish kernel takes the rest: the rows of the last, partial page, the carried rows and the block's own rows, in bf16
 // MMAs, and merges them with the partials.
@@ -108,12 +109,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
 }
 
 // Soft-max state of rows 8 n + 2 t + e (n < NR, e < 2) and the lane's share of the output: o[n][i] = (column CH g + 2 i,
-// rows e = 0, 1), (column CH g + 2 i + 1, rows e = 0, 1). o is relative to r, the lane's own sums l and lc to rl (log2 units).
+// rows e = 0, 1), (column CH g + 2 i + 1, rows e = 0, 1). The lane's own sums l and lc are relative to r, o to r + d (log2 units).
 template <int HD, int NR>
 struct RowState {
   static constexpr int NT = HD / 16;
   float o[NR][NT][4];
-  float r[NR][2], rl[NR][2], l[NR][2], lc[NR][2];
+  float r[NR][2], d[NR][2], l[NR][2], lc[NR][2];
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -122,37 +123,40 @@ struct RowState {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[n][i][e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) { r[n][e] = -INFINITY; rl[n][e] = -INFINITY; l[n][e] = 0.f; lc[n][e] = 0.f; }
+      for (int e = 0; e < 2; ++e) { r[n][e] = -INFINITY; d[n][e] = -INFINITY; l[n][e] = 0.f; lc[n][e] = 0.f; }
     }
   }
-  // Moves the references where one of the warp's x is too far above its row's; mx, ml: the lane's largest x per row with and
-  // without V's scale. The sums are plain floats: their reference may lie 60 below.
-  __device__ __forceinline__ void refer(const float (&mx)[NR][2], const float (&ml)[NR][2]) {
+  // Moves the references where one of the warp's scores asks for it; ml: the lane's largest per row, lv: log2 of V's scale.
+  __device__ __forceinline__ void refer(const float (&ml)[NR][2], float lv) {
     bool over = false;
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) over = over || mx[n][e] - r[n][e] > 15.f || ml[n][e] - rl[n][e] > 60.f;
+      for (int e = 0; e < 2; ++e) over = over || ml[n][e] - r[n][e] > 60.f || (ml[n][e] - r[n][e]) + lv - d[n][e] > 15.f;
     if (!__any_sync(0xffffffffu, over)) return;
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float m = max_over_g(mx[n][e]), k = max_over_g(ml[n][e]);
-        if (m - r[n][e] > 15.f) {
-          const float to = m - 10.f, f = ex2(r[n][e] - to);      // ex2(-inf) = 0 the first time
-          r[n][e] = to;
-#pragma unroll
-          for (int i = 0; i < NT; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
-        }
-        if (k - rl[n][e] > 60.f) {
-          const float f = ex2(rl[n][e] - k);
-          rl[n][e] = k;
+        const float k = max_over_g(ml[n][e]);
+        if (k - r[n][e] > 60.f) {
+          const float step = r[n][e] - k, f = ex2(step);        // ex2(-inf) = 0 the first time
+          r[n][e] = k;
+          d[n][e] += step;
           l[n][e] *= f;
           lc[n][e] *= f;
         }
+        const float x = (k - r[n][e]) + lv;
+        if (x - d[n][e] > 15.f) {
+          const float to = x - 10.f, f = ex2(d[n][e] - to);
+          d[n][e] = to;
+#pragma unroll
+          for (int i = 0; i < NT; ++i) { o[n][i][e] *= f; o[n][i][2 + e] *= f; }
+        }
       }
   }
+  // what turns a weight of the sum into one of raw V bytes (a weight that is not zero is 2^-126 at least: 2^120 passes no P' by)
+  __device__ __forceinline__ float factor(int n, int e, float lv) const { return ex2(fminf(lv - d[n][e], 120.f)); }
 };
 
 template <int HD, int NR>
@@ -171,7 +175,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
   float* const join = reinterpret_cast<float*>(sm0 + NW * STAGES * PGB);
   float* const tab = join + NW * RT * HD;
   __shared__ uint64_t bars[NW][STAGES];
-  __shared__ float4 ml_s[NW][RT];            // r, l, lc, rl
+  __shared__ float4 ml_s[NW][RT];            // d, r, l, lc
   __shared__ int scan_s[NW + 4];
   __shared__ int abort_s;
   volatile int& abort_flag = abort_s;
@@ -333,7 +337,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
               for (int n = 0; n < NR; ++n) mma_f16(w & 1 ? sw[n] : sv[n], a[0], a[1], a[2], a[3], qb[n][hf * CW + w][0], qb[n][hf * CW + w][1]);
             }
           const float lv = lg2(fmaxf(sc.y, 1.1754944e-38f));
-          float mx[NR][2], ml[NR][2];
+          float ml[NR][2];
 #pragma unroll
           for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -342,17 +346,18 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
               sv[n][e] = (sv[n][e] + sw[n][e]) * f;
               sv[n][2 + e] = (sv[n][2 + e] + sw[n][2 + e]) * f;
               ml[n][e] = fmaxf(sv[n][e], sv[n][2 + e]);
-              mx[n][e] = ml[n][e] + lv;
             }
-          st.refer(mx, ml);
+          st.refer(ml, lv);
           uint32_t pb[NR][2];
 #pragma unroll
           for (int n = 0; n < NR; ++n) {
-            const float r0 = st.r[n][0] - lv, r1 = st.r[n][1] - lv;
-            pb[n][0] = transpose8x8(pack_f16(ex2(sv[n][0] - r0), ex2(sv[n][1] - r1)));
-            pb[n][1] = transpose8x8(pack_f16(ex2(sv[n][2] - r0), ex2(sv[n][3] - r1)));
 #pragma unroll
-            for (int e = 0; e < 2; ++e) st.l[n][e] += ex2(sv[n][e] - st.rl[n][e]) + ex2(sv[n][2 + e] - st.rl[n][e]);
+            for (int e = 0; e < 4; ++e) sv[n][e] = ex2(sv[n][e] - st.r[n][e & 1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) st.l[n][e] += sv[n][e] + sv[n][2 + e];
+            const float f0 = st.factor(n, 0, lv), f1 = st.factor(n, 1, lv);
+            pb[n][0] = transpose8x8(pack_f16(sv[n][0] * f0, sv[n][1] * f1));
+            pb[n][1] = transpose8x8(pack_f16(sv[n][2] * f0, sv[n][3] * f1));
           }
 #pragma unroll
           for (int w = 0; w < CW; ++w) {
@@ -391,7 +396,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int lr = 8 * n + 2 * t + e, row = mt * RT + lr;
-          const float4 ml = make_float4(st.r[n][e], st.l[n][e], st.lc[n][e], st.rl[n][e]);
+          const float4 ml = make_float4(st.d[n][e], st.r[n][e], st.l[n][e], st.lc[n][e]);
           float* dst = KG > 1 ? join + (warp * RT + lr) * HD + CH * g : p.part_o + (slot * M + row) * HD + CH * g;
           if (KG == 1 && row >= M) continue;
 #pragma unroll
@@ -408,22 +413,24 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
           const int tile = idx / (RT * (HD / 4)), rem = idx - tile * RT * (HD / 4), r = rem / (HD / 4), d4 = (rem - r * (HD / 4)) * 4;
           const int row = (mt0 + tile) * RT + r;
           if (row >= M) continue;
-          float mg = -INFINITY, lg = -INFINITY;
-          for (int k = 0; k < KG; ++k) { mg = fmaxf(mg, ml_s[k * mw + tile][r].x); lg = fmaxf(lg, ml_s[k * mw + tile][r].w); }
-          const float mb = mg == -INFINITY ? 0.f : mg, lb = lg == -INFINITY ? 0.f : lg;
+          float lg = -INFINITY, mg = -INFINITY;
+          for (int k = 0; k < KG; ++k) lg = fmaxf(lg, ml_s[k * mw + tile][r].y);
+          const float lb = lg == -INFINITY ? 0.f : lg;
+          for (int k = 0; k < KG; ++k) mg = fmaxf(mg, ml_s[k * mw + tile][r].y - lb + ml_s[k * mw + tile][r].x);
+          const float mb = mg == -INFINITY ? 0.f : mg;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
           float l = 0.f, lc = 0.f;
           for (int k = 0; k < KG; ++k) {
             const int w = k * mw + tile;
             const float4 ml = ml_s[w][r];
-            const float f = ex2(ml.x - mb), fl = ex2(ml.w - lb);
+            const float fl = ex2(ml.y - lb), f = ex2(ml.y - lb + ml.x - mb);
             const float4 v = *reinterpret_cast<const float4*>(join + (w * RT + r) * HD + d4);
             acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
-            l = fmaf(fl, ml.y, l);
-            lc = fmaf(fl, ml.z, lc);
+            l = fmaf(fl, ml.z, l);
+            lc = fmaf(fl, ml.w, lc);
           }
           *reinterpret_cast<float4*>(p.part_o + (slot * M + row) * HD + d4) = acc;
-          if (d4 == 0) *reinterpret_cast<float4*>(p.part_ml + (slot * M + row) * 4) = make_float4(mg, l, lc, lg);
+          if (d4 == 0) *reinterpret_cast<float4*>(p.part_ml + (slot * M + row) * 4) = make_float4(mg, lg, l, lc);
         }
         // (the next segment's join writes come after the block-wide vote that ends its pages)
       }
@@ -465,8 +472,8 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
   float* const join = reinterpret_cast<float*>(smf);                          // [jrows][HD]: row tile mt of key group kg at mt + MT kg
   uint8_t* const stage = smf + static_cast<size_t>(jrows) * HD * sizeof(float);   // [2][FKEYS][KROW]
   float* const tab = reinterpret_cast<float*>(stage + 2 * FKEYS * KROW);      // cos | sin of the block rows
-  __shared__ float4 ml_s[16 * 8];            // [jrows] r, l, lc, rl
-  __shared__ float4 row_s[128];              // per row: o's reference, factor of o, share of the carried keys
+  __shared__ float4 ml_s[16 * 8];            // [jrows] d, r, l, lc
+  __shared__ float4 row_s[128];              // per row: o's reference against the sum's, factor of o, share of the carried keys, the sum's reference
   __shared__ int place_s[2 * FW];
   uint32_t flags = 0;
   const int L = clamped_len(p, s), Lr = L % PAGE;
@@ -558,7 +565,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
       __syncthreads();
       if (mt < mtiles) {
         for (int z0 = kg * 16; z0 < nf; z0 += KG * 16) {
-          float sv[1][4], mx[1][2];
+          float sv[1][4], ml[1][2];
 #pragma unroll
           for (int e = 0; e < 4; ++e) sv[0][e] = 0.f;
           const uint8_t* const k0 = stage + (z0 + g) * KROW + CH * t * 2;
@@ -581,21 +588,22 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
             sv[0][e] = zz < nf && (have_last || f0 + zz >= Lr) ? sv[0][e] * sl2 : -INFINITY;
           }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) mx[0][e] = fmaxf(sv[0][e], sv[0][2 + e]);
-          st.refer(mx, mx);
+          for (int e = 0; e < 2; ++e) ml[0][e] = fmaxf(sv[0][e], sv[0][2 + e]);
+          st.refer(ml, 0.f);
+          const float g0 = st.factor(0, 0, 0.f), g1 = st.factor(0, 1, 0.f);
           uint32_t pb[2], pc[2];
 #pragma unroll
           for (int k = 0; k < 2; ++k) {                      // key z0 + g + 8 k, rows 2 t and 2 t + 1
             const int z = f0 + z0 + g + 8 * k;
-            const float x = ex2(sv[0][2 * k] - st.r[0][0]), y = ex2(sv[0][2 * k + 1] - st.r[0][1]);
+            const float w[2] = {ex2(sv[0][2 * k] - st.r[0][0]), ex2(sv[0][2 * k + 1] - st.r[0][1])};
+            const float x = w[0] * g0, y = w[1] * g1;
             const uint32_t hi = pack_bf16(x, y);
             pb[k] = transpose8x8(hi);
             pc[k] = transpose8x8(rest_bf16(x, y, hi));
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float w = ex2(sv[0][2 * k + e] - st.rl[0][e]);
-              st.l[0][e] += w;
-              if (z >= Lr && z < Lr + c) st.lc[0][e] += w;
+              st.l[0][e] += w[e];
+              if (z >= Lr && z < Lr + c) st.lc[0][e] += w[e];
             }
           }
           const uint8_t* const v0 = stage + (FKEYS + z0 + 2 * t) * KROW + CH * g * 2;
@@ -621,7 +629,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
 #pragma unroll
         for (int i = 0; i < NT; i += 2)
           *reinterpret_cast<float4*>(dst + 2 * i) = make_float4(st.o[0][i][e], st.o[0][i][2 + e], st.o[0][i + 1][e], st.o[0][i + 1][2 + e]);
-        if (g == 0) ml_s[at] = make_float4(st.r[0][e], l, lc, st.rl[0][e]);
+        if (g == 0) ml_s[at] = make_float4(st.d[0][e], st.r[0][e], l, lc);
       }
     }
   }
@@ -645,32 +653,27 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
   for (int r0 = warp * 4; r0 < rows; r0 += FW * 4) {
     const int r = r0 + (lane >> 3), k0 = lane & 7;
     const bool there = r < rows;
-    const float4 none = make_float4(-INFINITY, 0.f, 0.f, -INFINITY);
+    const float4 none = make_float4(-INFINITY, -INFINITY, 0.f, 0.f);
     const float4 own = there && k0 < KG ? ml_s[((r >> 3) + MT * k0) * 8 + (r & 7)] : none;
-    float mg = own.x, lg = own.w;
-    for (int k = k0; there && k < n_parts; k += 8) {
-      const float4 ml = recs[static_cast<size_t>(k) * M + r];
-      mg = fmaxf(mg, ml.x);
-      lg = fmaxf(lg, ml.w);
-    }
+    float lg = own.y;
+    for (int k = k0; there && k < n_parts; k += 8) lg = fmaxf(lg, recs[static_cast<size_t>(k) * M + r].y);
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
-      mg = fmaxf(mg, __shfl_xor_sync(0xffffffffu, mg, o));
-      lg = fmaxf(lg, __shfl_xor_sync(0xffffffffu, lg, o));
-    }
-    const float mb = mg == -INFINITY ? 0.f : mg, lb = lg == -INFINITY ? 0.f : lg, wl = ex2(own.w - lb);
-    float l = own.y * wl, lc = own.z * wl;
+    for (int o = 1; o < 8; o <<= 1) lg = fmaxf(lg, __shfl_xor_sync(0xffffffffu, lg, o));
+    const float lb = lg == -INFINITY ? 0.f : lg, wl = ex2(own.y - lb);
+    float l = own.z * wl, lc = own.w * wl, mg = own.y - lb + own.x;
     for (int k = k0; there && k < n_parts; k += 8) {
       const float4 ml = recs[static_cast<size_t>(k) * M + r];
-      l = fmaf(ex2(ml.w - lb), ml.y, l);
+      l = fmaf(ex2(ml.y - lb), ml.z, l);
+      mg = fmaxf(mg, ml.y - lb + ml.x);
     }
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
       l += __shfl_xor_sync(0xffffffffu, l, o);
       lc += __shfl_xor_sync(0xffffffffu, lc, o);
+      mg = fmaxf(mg, __shfl_xor_sync(0xffffffffu, mg, o));
     }
-    const float inv_l = 1.f / l;
-    if (there && k0 == 0) row_s[r] = make_float4(mb, inv_l * ex2(mg - lg), lc * inv_l, 0.f);   // (o's reference against the sum's)
+    const float mb = mg == -INFINITY ? 0.f : mg, inv_l = 1.f / l, half = ex2(0.5f * mb);     // (2^mb alone may pass float's range)
+    if (there && k0 == 0) row_s[r] = make_float4(mb, inv_l * half * half, lc * inv_l, lb);
   }
   __syncthreads();
 
@@ -681,24 +684,26 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
   const float* const parts = p.part_o + (first_part * M + row0) * HD + lane * V;
 #pragma unroll 1
   for (int r0 = warp; r0 < rows; r0 += FW * ROWS) {
-    float acc[ROWS][V], mb[ROWS];
+    float acc[ROWS][V], mb[ROWS], lb[ROWS];
     int rr[ROWS];
 #pragma unroll
     for (int b = 0; b < ROWS; ++b) {
       rr[b] = min(r0 + FW * b, rows - 1);
       mb[b] = row_s[rr[b]].x;
+      lb[b] = row_s[rr[b]].w;
 #pragma unroll
       for (int e = 0; e < V; ++e) acc[b][e] = 0.f;
     }
 #pragma unroll 1
     for (int k0 = 0; k0 < n_parts; k0 += PARTS) {
-      float v[ROWS][PARTS][V], x[ROWS][PARTS];
+      float v[ROWS][PARTS][V];
+      float2 x[ROWS][PARTS];                 // d, r
 #pragma unroll
       for (int b = 0; b < ROWS; ++b)
 #pragma unroll
         for (int u = 0; u < PARTS; ++u) {
           const size_t at = static_cast<size_t>(min(k0 + u, n_parts - 1)) * M + rr[b];
-          x[b][u] = recs[at].x;
+          x[b][u] = *reinterpret_cast<const float2*>(recs + at);
           if constexpr (V == 4) { const float4 f = ld_now(reinterpret_cast<const float4*>(parts + at * HD)); v[b][u][0] = f.x; v[b][u][1] = f.y; v[b][u][2] = f.z; v[b][u][3] = f.w; }
           else { const float2 f = ld_now(reinterpret_cast<const float2*>(parts + at * HD)); v[b][u][0] = f.x; v[b][u][1] = f.y; }
         }
@@ -706,7 +711,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
       for (int b = 0; b < ROWS; ++b)
 #pragma unroll
         for (int u = 0; u < PARTS; ++u) {
-          const float w = k0 + u < n_parts ? ex2(x[b][u] - mb[b]) : 0.f;
+          const float w = k0 + u < n_parts ? ex2(x[b][u].y - lb[b] + x[b][u].x - mb[b]) : 0.f;
 #pragma unroll
           for (int e = 0; e < V; ++e) acc[b][e] = fmaf(w, v[b][u][e], acc[b][e]);
         }
@@ -716,7 +721,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
 #pragma unroll
       for (int b = 0; b < ROWS; ++b) {
         const int at = ((rr[b] >> 3) + MT * k) * 8 + (rr[b] & 7);
-        const float f = ex2(ml_s[at].x - mb[b]);
+        const float f = ex2(ml_s[at].y - lb[b] + ml_s[at].x - mb[b]);
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[b][e] = fmaf(f, join[at * HD + lane * V + e], acc[b][e]);
       }

@@ -412,6 +412,8 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
           for (int e = 0; e < 2; ++e) { unpack_bf16(raw[e], lo + 8 * e); unpack_bf16(raw[2 + e], hi + 8 * e); }
           if (rotate) rotate_chunk<16>(lo, hi, tab + (tok - i0) * HD + 16 * c, HD / 2);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { lo[e] *= sl2; hi[e] *= sl2; }       // the products are log2-scores
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) a = fmaxf(a, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
@@ -464,8 +466,9 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         tc_fence_after();
         const uint32_t s_at = t_lane + COL_S + buf * NROW;
         const float4 pg = page_s[buf * TPAGES + (key >> 4)];
-        const float kf = pg.x * sl2, vs = pg.y, lv = pg.z;
-        auto score = [&](uint32_t s, int q, float add) { return fmaf(__uint_as_float(s), q_s[q] * kf, add); };    // log2-score of row q
+        const float kf = pg.x, vs = pg.y, lv = pg.z;
+        // log2-score of row q, and more; the factor is a power of two, so the score itself is exact and the weights see the same one
+        auto score = [&](uint32_t s, int q, float add) { return fmaf(__uint_as_float(s), q_s[q] * kf, add); };
         const float* const ref = lv > -INFINITY ? nr : none_s;               // a masked key: 2^-inf
         const bool starts = i < 2;             // the group's first tile of the segment sets the references
         if (m >= PBUF) wait_done(m - PBUF);    // the product of the weights that had the buffer before
@@ -524,19 +527,6 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             // some weight times V's scale outgrows f16: new references where they are needed, O and the sums scaled to them (less
             // what this tile has just added; a sum that became infinite starts again from zero: the row's new reference is more
             // than 2^100 above everything that was in it), P again
-#pragma unroll 1
-            for (int c = 0; c < npad; c += 16) {
-              uint32_t s[16];
-              tmem_ld16_nowait(s_at + c, s);
-              tmem_wait_ld(s);
-              float cm = 0.f;
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float m = warp_max(score(s[e], c + e, lv));
-                cm = lane == e ? m : cm;
-              }
-              if (lane < 16) xs[(warp & 3) * NROW + c + lane] = cm;
-            }
             if (!starts) {
 #pragma unroll
               for (int c = 0; c < NROW; c += 16) {
@@ -552,13 +542,38 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 }
               }
             }
-            sync_group(grp);
-            if ((tid & 127) < npad) {
-              const int q = tid & 127;
-              const float mx = fmaxf(fmaxf(xs[q], xs[NROW + q]), fmaxf(xs[2 * NROW + q], xs[3 * NROW + q])), old = starts ? -INFINITY : -nr[q];
-              const bool up = mx - old > 15.f;
+            // (scores beyond 2^22 leave no room beside them for log2 s_V: there the row's largest score itself is the reference)
+            const int q = tid & 127;
+            float mx = 0.f, raw = 0.f;
+            bool huge = false;
+#pragma unroll 1
+            for (int kind = 0;; kind = 1) {
+              const float add = kind == 0 || lv == -INFINITY ? lv : 0.f;
+#pragma unroll 1
+              for (int c = 0; c < npad; c += 16) {
+                uint32_t s[16];
+                tmem_ld16_nowait(s_at + c, s);
+                tmem_wait_ld(s);
+                float cm = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const float m = warp_max(score(s[e], c + e, add));
+                  cm = lane == e ? m : cm;
+                }
+                if (lane < 16) xs[(warp & 3) * NROW + c + lane] = cm;
+              }
+              sync_group(grp);
+              if (q < npad) {
+                raw = fmaxf(fmaxf(xs[q], xs[NROW + q]), fmaxf(xs[2 * NROW + q], xs[3 * NROW + q]));
+                if (kind == 0) { mx = raw; huge = fabsf(mx) >= 4194304.f && mx > -INFINITY; }
+              }
+              if (kind == 1 || !vote_group(grp, huge)) break;
+            }
+            if (q < npad) {
+              const float old = starts ? -INFINITY : -nr[q];
+              const bool up = huge ? raw > old : mx - old > 15.f;
               // (a first tile of bad pages alone leaves the row without a reference: the first key that counts overflows, and sets it)
-              const float to = up ? mx - 10.f : old;
+              const float to = !up ? old : huge ? raw : mx - 10.f;
               fs[q] = starts ? 0.f : up ? ex2(old - to) : 1.f;
               nr[q] = -to;
             }
@@ -657,7 +672,7 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
           sum += ((y[q] + y[NROW + q]) + (y[2 * NROW + q] + y[3 * NROW + q])) * f_s[NROW + q];
           r = fmaxf(r, -nr_s[NROW + q]);
         }
-        *reinterpret_cast<float4*>(p.part_ml + (slot * M + row0 + q) * 4) = make_float4(r, sum, 0.f, r);
+        *reinterpret_cast<float4*>(p.part_ml + (slot * M + row0 + q) * 4) = make_float4(0.f, r, sum, 0.f);
       }
       tc_fence_before();
       sync_workers();                          // references, sums and the buffer have been read

@@ -17,7 +17,7 @@ struct Kv8Params {
   int unit, setup;                           // work line: pages per unit; what it costs to begin a segment, in units
   int line_blocks;                           // how many stretches the work line is cut into
   int run_ahead;                             // finish kernel: what it reads before its wait is older than the paged kernel
-  float *part_o, *part_ml;                   // [slot][M][hd], [slot][M][4]: r, l, l_carry, rl
+  float *part_o, *part_ml;                   // [slot][M][hd], [slot][M][4]: d, r, l, l_carry (the sums are relative to r, o to r + d)
   uint32_t* status;
 };
 

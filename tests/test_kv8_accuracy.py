@@ -224,3 +224,48 @@ def test_a_row_that_is_not_finite_or_huge_leaves_the_others_alone(name, value, f
     rows = _compare_all_but(ctx, st, args, odd)
     assert value == 3e38 or not np.isfinite(rows).any()          # what has no score has no output, in every kernel
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("flags", [0, 2], ids=["", "plain_fma"])
+@pytest.mark.parametrize("k", [6, 10, 13, 16, 17, 18, 19, 20, 22, 26, 32, 40, 60])
+@pytest.mark.parametrize("name", MIXED)
+def test_outputs_of_huge_scores_stay_among_the_values(name, k, flags):
+    """Scores of up to 2^60: the weights' differences are lost in their rounding, their sum is not. Every output lies between the
+    least and the largest value of its column, but for the weights' and its own rounding, and a row whose largest score leads
+    by far is that key's value."""
+    T = _gpu()
+    case = MIXED[name]
+    ctx, st, args = _run(case, flags, seed=9)
+    layer, q, kb, vb, _, S, use, out, mass = args
+    args[2].mul_(2.0 ** k)
+    st.carry_kv[:, :, :, 0] *= 2.0 ** k
+    st.kv_scale[..., 0] *= 2.0 ** k
+    ctx.block_attn(*args)
+    v = T._values
+    o, m = v(out), v(mass)
+    assert np.isfinite(o).all() and (m >= 0).all() and (m <= 1 + 2.0 ** -10).all()
+    rep, W, n_led = case["n_q"] // case["n_kv"], case["W"], 0
+    pool, scale, car = np.nan_to_num(v(st.kv_pool)[0]), np.nan_to_num(v(st.kv_scale)[0]), np.nan_to_num(v(st.carry_kv)[0])
+    for s in range(S):
+        L, c = int(st.committed_len[s]), int(st.carry_len[s])
+        ids = st.block_table[s, :(L + 15) // 16].cpu().numpy()
+        pos = (L + np.arange(W))[:, None]
+        qs, ks = ref.rope(v(q)[s], pos, 1e6), ref.rope(v(kb)[s], pos, 1e6)
+        for h in range(case["n_kv"]):
+            body = [(pool[ids, h, i] * scale[ids, h, i][:, None, None]).reshape(-1, case["hd"])[:L] for i in range(2)]
+            keys = np.concatenate([body[0], car[s, h, 0, :c], ks[:, h]])
+            vals = np.concatenate([body[1], car[s, h, 1, :c], v(vb)[s, :, h]])
+            # f16 weights: each off by 2^-11, their sum of products by that of the largest |value|; then the output's own rounding
+            slack = (2.0 ** -10 + 2.0 ** -8) * np.abs(vals).max(0)
+            for g in range(h * rep, (h + 1) * rep):
+                assert (o[s, :, g] >= vals.min(0) - slack).all() and (o[s, :, g] <= vals.max(0) + slack).all()
+                sc = qs[:, g] @ keys.T / np.sqrt(case["hd"])
+                room = 2 * 2.0 ** -7 * (np.abs(qs[:, g]) @ np.abs(keys).T).max(1) / np.sqrt(case["hd"]) + 40      # q's and the key's rounding at two keys
+                best = sc.argmax(1)
+                lead = sc.max(1) - np.partition(sc, -2, 1)[:, -2] if sc.shape[1] > 1 else np.full(W, np.inf)
+                for i in np.nonzero(lead > room)[0]:
+                    n_led += 1
+                    assert (np.abs(o[s, i, g] - vals[best[i]]) <= slack).all()
+    assert n_led > 0 or k < 10 or case["W"] > 1
+    ctx.close()
