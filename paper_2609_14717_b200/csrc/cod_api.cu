@@ -730,7 +730,7 @@ int cod_selftest_expire_wait(cod_ctx* c, int on) {
 int cod_profile_enable(cod_ctx* c, uint32_t class_mask) {
   if (!c) return COD_ERR_INVALID_ARG;
   const uint32_t mask = class_mask & ((1u << COD_K_CLASSES) - 1u);
-  if (mask && (other_device(c) || !make_prof(c))) return COD_ERR_CUDA;
+  if (mask && !c->prof_ev && (other_device(c) || !make_prof(c))) return COD_ERR_CUDA;
   c->prof_mask = mask;
   c->prof_n = 0;
   return COD_OK;
