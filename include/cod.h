@@ -96,7 +96,11 @@ enum cod_mode {
                           and block rows keep the context's element type. Appending to a page that already holds rows
                           may raise its scale; the held bytes are then rescaled, which is exact except where they fall
                           into e4m3's subnormals (below 2^-6 of the new scale: one more rounding, at most 2^-10 of it).
-                          NaN stays NaN, an infinity saturates at 448 * scale and does not raise the scale. */
+                          NaN stays NaN, an infinity saturates at 448 * scale and does not raise the scale.
+                          Attention on such a cache reads the bytes exactly, with sums and outputs in float. bf16 contexts
+                          keep eight significant bits at least of q and of the block's keys after their rotation (each row of q by itself;
+                          elements below 2^-10 of their row's largest to 2^-18 of that) and the soft-max weights to f16
+                          (eleven bits); float contexts and COD_F_NO_TENSOR_CORES keep the weights in float */
 
 /* bits of the sticky device status word */
 #define COD_DEV_BAD_TOKEN 1u      /* a token id outside [0, vocab) was met (treated as id 0) */

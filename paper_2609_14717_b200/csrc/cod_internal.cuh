@@ -29,6 +29,15 @@ __device__ __forceinline__ void cod_pdl_prologue() {
   if (gridDim.x * gridDim.y * gridDim.z <= 1024u) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
+// cos and sin of pos * freq. The angle is formed and reduced modulo 2*pi in double, so positions of tens of thousands lose
+// nothing in float.
+__device__ __forceinline__ void cod_sincos_at(int pos, double freq, float& sn, float& cs) {
+  const double two_pi = 6.283185307179586476925286766559;
+  double a = static_cast<double>(pos) * freq;
+  a -= two_pi * rint(a / two_pi);
+  sincosf(static_cast<float>(a), &sn, &cs);
+}
+
 // Drops one 128-byte line (address aligned to 128 bytes) from L2 without writing it back: for scratch data that
 // has been read for the last time. Whatever is read there before the next write is indeterminate, and the caller
 // orders the drop after every read of the line: the readers synchronise with the dropping thread first, and the

@@ -32,9 +32,10 @@
 // moves on by a block, a pair or both, so no two meet.
 // The finish kernel takes the rest: the rows of the last, partial page, the carried rows and the block's own rows, in bf16
 // MMAs, and merges them with the partials.
-// Measured, both kernels: one token for each of 32 requests of 512 to 8192 tokens (285 MB) 56 us = 5.0 TB/s, where a kernel
-// that only streams the same boxes takes 52 to 58; one token of one request 10 us, three dependent trips to memory in each
-// kernel. The pages' copies leave L2 first (evict-first): 60 us without.
+// Measured, both kernels, captured in a graph: one token for each of 32 requests of 512 to 8192 tokens (285 MB) 57.6 us =
+// 4.9 TB/s, where this grid with its rings of boxes and nothing else (every warp only waits for each box and asks for the next)
+// takes 52 to 58; one token of one request 10.6 us, three dependent trips to memory in each kernel. The pages' copies leave
+// L2 first (evict-first): 4 us more without.
 #include "kv8_common.cuh"
 #include "tc_common.cuh"
 
@@ -241,7 +242,7 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
         const int half = HD / 2;
         for (int e = threadIdx.x; e < p.W * half; e += NW * 32) {
           const int i = e / half, j = e - i * half;
-          sincos_at(cur.L + i, p.inv_freq[j], tab[i * HD + half + j], tab[i * HD + j]);
+          cod_sincos_at(cur.L + i, p.inv_freq[j], tab[i * HD + half + j], tab[i * HD + j]);
         }
         __syncthreads();
         tab_s = cur.s;
@@ -451,7 +452,8 @@ k_attn_kv8(const __grid_constant__ CUtensorMap map_pool, const Kv8Params p) {
 // SMs its last blocks leave free.
 // Keys and values are bf16 (a block's keys are rounded to it after their rotation); q and the weights enter as two bf16 terms
 // each, so that of a short context no more is lost than the keys' and the output's rounding (one term each: 0.0026 relative
-// instead of 0.0020, where rounding the output alone is 0.0017; 1 us at batch 32, block 16).
+// instead of 0.0020, where rounding the output alone is 0.0017; 1 us at batch 32, block 16). The 128-wide forms spill 8 to 16
+// bytes at the 128 registers that two blocks per SM leave.
 constexpr int FW = 8, FKEYS = 64;              // warps; keys staged at a time
 __device__ __forceinline__ uint32_t rest_bf16(float x, float y, uint32_t hi) {      // what packing x and y into `hi` left
   return pack_bf16(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xFFFF0000u));
@@ -497,7 +499,7 @@ k_attn_kv8_finish(const Kv8Params p, int tpb, __nv_bfloat16* __restrict__ out, f
     const int half = HD / 2;
     for (int e = threadIdx.x; e < p.W * half; e += FW * 32) {
       const int i = e / half, j = e - i * half;
-      sincos_at(L + i, p.inv_freq[j], tab[i * HD + half + j], tab[i * HD + j]);
+      cod_sincos_at(L + i, p.inv_freq[j], tab[i * HD + half + j], tab[i * HD + j]);
     }
     __syncthreads();
   }
@@ -755,7 +757,10 @@ int launch(cod_ctx* c, int layer, const void* q, const void* kb, const void* vb,
   p.max_pages = f.max_pages_per_seq; p.max_batch = f.max_batch; p.cap = c->carry_cap;
   p.S = S;
   p.part_o = c->attn_o; p.part_ml = c->attn_ml; p.status = c->status;
-  const int nr = HD == 128 || M <= 8 ? 1 : 2;  // row tiles per warp (more than eight rows of head size 128: the other kernel)
+  // row tiles per warp (more than eight rows of head size 128: the other kernel). Head size 64 has this form for every row count,
+  // the tcgen05 tile being 128 columns wide: 4, 16, 64, 128 rows take 43, 75, 186, 368 us at batch 32, 12, 14, 21, 35 for one
+  // request of 2048 tokens; the plain-FMA kernel 319 to 2988 and 61 to 191.
+  const int nr = HD == 128 || M <= 8 ? 1 : 2;
   const bool tcgen = cod_attn_kv8_tc_fits(c);
   p.unit = tcgen ? cod_attn_kv8_tc_unit() : 1;
   p.setup = tcgen ? cod_attn_kv8_tc_setup() : 0;

@@ -24,10 +24,11 @@
 // the MMAs of either product (an MMA costs its issuer some 60 cycles to set up: twelve per tile from one warp held the others
 // up). More than 64 rows are two row groups: blocks 2 i and 2 i + 1 walk the same stretch of keys, so the second read of a
 // page finds it in L2.
-// Measured, with the finish kernel: batch 32 of 512 to 8192 tokens, block 16: 94 us (285 MB: 3.0 TB/s); 4 x 32K, block 32: 124 us;
-// one request of 2048 tokens, block 16: 16 us. A tile of 128 keys takes about 1900 cycles, and as many wavefronts of shared
-// memory (998 of loads and stores, 640 of MMA operands, 256 of copies; V's way through f16 is the largest part); a segment
-// costs about six tiles more to begin and end.
+// Measured, with the finish kernel, captured in a graph at 1965 MHz: batch 32 of 512 to 8192 tokens, block 16: 94.7 us (285 MB:
+// 3.0 TB/s); 4 x 32K, block 32: 129.6 us; one request of 2048 tokens, block 16: 16.3 us. (Repeated for a second and more the card
+// reaches its power limit, the clock falls to 1860 and 1815 MHz and the first two take 100 and 141 us.) A tile of 128 keys takes about
+// 2100 cycles, and as many wavefronts of shared memory (1062 of loads and stores, 768 of MMA operands, 256 of copies; V's way
+// through f16 is the largest part); a segment costs about six tiles more to begin and end.
 // Work is cut as in k_attn_kv8.cu, in tiles of eight pages. Pages behind the end of a segment, and bad ones, are masked.
 #include "kv8_common.cuh"
 #include "tc_common.cuh"
@@ -401,7 +402,7 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         if (rotate) {
           for (int e = tid; e < nt * (HD / 2); e += WORKERS) {
             const int i = e / (HD / 2), j = e - i * (HD / 2);
-            sincos_at(k.L + i0 + i, p.inv_freq[j], tab[i * HD + HD / 2 + j], tab[i * HD + j]);
+            cod_sincos_at(k.L + i0 + i, p.inv_freq[j], tab[i * HD + HD / 2 + j], tab[i * HD + j]);
           }
           sync_workers();
         }
@@ -697,9 +698,10 @@ k_attn_kv8_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 
 }  // namespace
 
-// The register form has one row tile of eight in its MMAs and is nearer to the memory's rate with that (8 rows: 63 against
-// 76 us at batch 32, 55 against 64 at 4 x 32K, 11 against 14 at batch 1); with more rows it falls behind (16 rows: 96 against 78,
-// 68 against 64, 14.0 against 13.7; 32 rows: 149 against 80, 115 against 65, 18 against 14).
+// The register form has one row tile of eight in its MMAs and is nearer to the memory's rate with that (8 rows: 61 against
+// 78 us at batch 32, 55 against 66 at 4 x 32K, 14 against 16 for one request); with a second tile it falls behind, be it full or not
+// (9 rows: 111 against 80, 94 against 67, equal for one request; 12: 110 against 78, 94 against 66; 16: 113 against 78, 94 against 67;
+// 32: 180 against 80, 168 against 68, 20 against 16).
 bool cod_attn_kv8_tc_fits(const cod_ctx* c) {
   const int M = c->cfg.block * (c->cfg.n_q_heads / c->cfg.n_kv_heads);
   return c->cfg.head_dim == HD && M > 8 && M <= 2 * NROW;

@@ -76,7 +76,7 @@ template <> struct Raw8<float> {
 // (A page that occurs again after another page's rows would have two owners unseen: finding those takes a pass over the whole map.)
 // LONG: what bounds a long map is how many rows are on their way, so registers give way to a fourth block per SM (bf16; 25,000
 // rows of five layers: 142 us, with three blocks 152, with five, which spill, 147; its bytes at the rate of a plain copy: 132).
-// A short map fits the machine at once and keeps them (a round's rows at batch 32: 7.5 us).
+// A short map fits the machine at once and keeps them (a round's rows at batch 32: 7.5 us). Four blocks spill 8 bytes.
 template <typename T, int HD, bool LONG>
 __global__ void __launch_bounds__(APPEND_WARPS * 32, !LONG ? 1 : sizeof(T) == 2 ? 4 : 2)
 k_kv8_append(const T* __restrict__ J, const int* __restrict__ slot, int n_rows, int n_kv, int n_pages, int chunk,
@@ -204,7 +204,9 @@ int launch_append(cod_ctx* c, const void* J, const int32_t* slot, int n_rows, co
   const cod_config& f = c->cfg;
   // Rows per block: a page's rows are one task per (head, K|V), so blocks of 16 rows give the warps of a long prompt their
   // pages with few empty blocks; short maps are dealt finer, so that the machine fills. Five layers, 16 against 4 rows per block:
-  // 2048 rows 14.8 and 19.3 us, 1024 rows 9.0 and 10.2, 512 rows 6.5 and 6.6, but 13.3 and 7.2 for 272 rows of 32 requests.
+  // 2048 rows 14.8 and 19.3 us, 1024 rows 9.0 and 10.2, 512 rows 6.5 and 6.6, but 13.3 and 7.2 for 272 rows of 32 requests. Floats
+  // agree (2048 rows: 19.4 and 35.0). The bounds are those of five layers: with one, prompts of 512 to 2048 rows take 7.5 to 8.2 us
+  // (floats 9 to 12) where blocks of 16 rows took 6.2, and 272 rows of 32 requests 6.2 where those took 10.3.
   const long long work = static_cast<long long>(n_rows) * f.n_layers;
   const bool is_long = work > 24ll * c->n_sm;
   const int chunk = is_long ? 16 : work > 8ll * c->n_sm ? 4 : 1;

@@ -9,7 +9,7 @@
 // A sequence whose numbers are out of range (a negative length, held beyond the table) is refused: nothing of it changes.
 //
 // A few words per page and row: bound by latency (dependent trips to L2), not by bytes (release and reserve of a round at
-// batch 32: 8.4 us on the device; admission of 64 prompts with 60,000 row slots: 11.6 us). One launch: every block
+// batch 32: 8.9 us on the device; admission of 64 prompts with 60,000 row slots: 12.6 us). One launch: every block
 // computes the prefix sums of the whole batch for itself from unchanged inputs (S words) and fills its share of the
 // pages and rows; the block that finishes last, known by a ticket, writes held, n_free and the lengths, which all the
 // others have read by then. Sizes the blocks cannot know (the total of the needs) only bound loops.
@@ -268,7 +268,7 @@ PagesArgs common_args(cod_ctx* c, const cod_pages* pages, const int32_t* len_in,
 }
 
 // blocks for `items` pages or rows at most: one a thread, two blocks per SM at most (a row's slot is a chain of dependent reads;
-// admission of 64 prompts: 11.6 us, with one block per SM 13.9, with four rows a thread 15.8)
+// admission of 64 prompts: 12.6 us; when it took 11.6, one block per SM took 13.9, four rows a thread 15.8)
 int blocks_for(const cod_ctx* c, long long items) {
   const long long b = (items + PT - 1) / PT;
   return static_cast<int>(b < 1 ? 1 : b > 2 * c->n_sm ? 2 * c->n_sm : b);

@@ -12,19 +12,14 @@ struct RopeTabs {
   float* rope_blk;
 };
 __device__ __forceinline__ void rope_entry(const RopeTabs& t, int r, int j, int pos_win, int pos_blk) {
-  const double two_pi = 6.283185307179586476925286766559;
   const double f = t.inv_freq[j];
   float sn, cs;
   if (t.rope_win) {
-    double a = static_cast<double>(pos_win) * f;
-    a -= two_pi * rint(a / two_pi);
-    sincosf(static_cast<float>(a), &sn, &cs);
+    cod_sincos_at(pos_win, f, sn, cs);
     t.rope_win[r * 2 * t.half + j] = cs; t.rope_win[r * 2 * t.half + t.half + j] = sn;
   }
   if (t.rope_blk) {
-    double b = static_cast<double>(pos_blk) * f;
-    b -= two_pi * rint(b / two_pi);
-    sincosf(static_cast<float>(b), &sn, &cs);
+    cod_sincos_at(pos_blk, f, sn, cs);
     t.rope_blk[r * 2 * t.half + j] = cs; t.rope_blk[r * 2 * t.half + t.half + j] = sn;
   }
 }

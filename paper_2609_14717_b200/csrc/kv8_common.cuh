@@ -76,13 +76,6 @@ __device__ __forceinline__ void tma_page(uint32_t dst, const CUtensorMap* map, i
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3}], [%4], %5;"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(bar), "l"(pol) : "memory");
 }
-// cos and sin of pos * freq, the angle reduced in double
-__device__ __forceinline__ void sincos_at(int pos, double freq, float& sn, float& cs) {
-  const double two_pi = 6.283185307179586476925286766559;
-  double a = static_cast<double>(pos) * freq;
-  a -= two_pi * rint(a / two_pi);
-  sincosf(static_cast<float>(a), &sn, &cs);
-}
 // N words from global memory (8 or 16 bytes, aligned to their size)
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
