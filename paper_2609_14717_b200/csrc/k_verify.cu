@@ -78,7 +78,7 @@ k_verify_accept(const int32_t* __restrict__ draft, const int32_t* __restrict__ t
       missing |= __reduce_or_sync(0xffffffffu, p < m ? no_place : 0u);
     }
     if (lane == 0) {
-      // an accepted row without a page (cod_pages_reserve refused the sequence): it sits this round out and nothing of it changes.
+      // an accepted row without a page (cod_pages_reserve refused the sequence): it sits the round out and nothing of it changes.
       // Its next block is drafted from its window's first token, i.e. it is the present one again.
       const bool waits = missing != 0;
       flags |= missing;
